@@ -312,6 +312,74 @@ int iso_quantize_rows_fp8(iso_ctx *ctx, const void *x, int rows, int cols, void 
 int iso_gemm_fp8(iso_ctx *ctx, const void *a8, const float *sa, const void *w8, const float *sw, void *c,
                  int M, int N, int K, void *stream);
 
+/* A paged key/value cache held in 4 bits, for answering after the prefill: many requests of any length, each over pages of its
+ * own, 4.25 bits per element instead of 16 or 32.  (Section 4.1 keeps the cache in 8 bits; 32 elements that share a scale carry a
+ * 4-bit type of the CDNA4 matrix cores.)
+ *   Format.  Blocks of 32 neighbouring elements of a head share a scale 2^(s-127), s one byte; an element is a sign and one of
+ *   0, 0.5, 1, 1.5, 2, 3, 4, 6 (E2M1: sign, two exponent bits, one fraction bit), two elements a byte, the first in the low four
+ *   bits.  Writing a block x: e = least integer with max|x| <= 7 * 2^e, not below -125 nor above 125; s = e + 127; each element the
+ *   nearest of the values times 2^e, ties to the even code.  An element is off by at most 2^e, i.e. less than 2/7 of the block's
+ *   largest.  A block with a NaN or an infinity gets s = 255 and stands for 32 NaN.
+ *   Layout.  k, v [n_pages, nkv, page, d/2] bytes; k_scale, v_scale [n_pages, nkv, page, d/32] bytes.  A token's slot is its page's
+ *   number * page + its place in the page.  Both context types (ISO_F32, ISO_BF16) read and write it; nothing in it depends on the
+ *   type.  The library never looks at a page that no table or slot names.
+ * Pointers are 16-byte aligned, int pointers 4-byte (else ISO_ERR_SHAPE).  These calls use nothing of the context but its
+ * configuration and rotary table, run on any stream of the context's device (which has to be current, else ISO_ERR_HIP), and may
+ * be recorded into a HIP graph and replayed. */
+typedef struct {
+    void *k, *v;             /* element codes                                                            */
+    void *k_scale, *v_scale; /* scale bytes                                                              */
+    int n_pages;             /* n_pages * page below 2^31                                                */
+    int page;                /* tokens per page: 16, 32, 64, 128 or 256                                  */
+} iso_kv4;
+
+/* Block tables, positions and slots of one step, from the requests' lengths, all on the device.  Request i has cached[i] tokens
+ * in the cache and fresh[i] new ones in this step (both >= 0; a negative one counts as 0; sums below 2^31).
+ *   row_start [n_seqs+1]  first row of each request in the step's tensors (sum of the fresh tokens before it), and the sum
+ *   kv_len    [n_seqs]    cached + fresh
+ *   block_table [n_seqs, max_pages]  entry (i, c) = page of request i's tokens c * page ..; the entries of the cached tokens are read,
+ *                         those of further pages that the new tokens need are taken from free_pages in order (request after
+ *                         request), the others are left alone.  Past the end of free_pages: -1.
+ *   free_head [1] or NULL (0): first entry of free_pages [n_free] that is free; free_next [1]: free_head + pages needed.  More than
+ *                         n_free means that the list was too short.  A captured step chains them from one replay to the next.
+ *   positions, slots [max_rows]  position and slot of every row; the slot is -1 where the request has no page (list too short,
+ *                         table too narrow), both are -1 behind the last row.  Rows past max_rows are not written (row_start says how many
+ *                         there are).
+ * Outputs must not overlap inputs (ISO_ERR_SHAPE where kv_len is cached or fresh, or free_next is free_head).
+ * Errors: NULL, n_seqs outside [1, 4096], n_free < 0, max_pages < 1 or max_rows < 1, an unknown page size (ISO_ERR_SHAPE). */
+int iso_block_tables(iso_ctx *ctx, const int *cached, const int *fresh, int n_seqs, int page, const int *free_pages, int n_free,
+                     const int *free_head, int *block_table, int max_pages, int *row_start, int *kv_len, int *positions, int *slots,
+                     int max_rows, int *free_next, void *stream);
+
+/* iso_rope_kv_write into pages: qkv [T, (nq + 2 nkv) * d]; row t is rotated for positions[t] and its k and v are written, in 4 bits,
+ * to slots[t].  The rotated q goes to q_out [T, nq, d], or back into qkv where q_out is NULL.  k is rotated in 64 bits (from the same
+ * fp32 table), so that its codes are those of the exact value.  A row whose position is outside [0, max_seq) is left alone, q too; one
+ * whose slot is not in the cache has only its q rotated.  Slots must differ from one another (else that slot's content is undefined).
+ * Errors: NULL, T < 1, a cache that is none (ISO_ERR_SHAPE). */
+int iso_rope_kv4_write(iso_ctx *ctx, void *qkv, void *q_out, const iso_kv4 *cache, const int *positions, const int *slots, int T,
+                       void *stream);
+/* Rows k, v [T, nkv, d] of cfg.dtype, as a prefill leaves them in its cache, into slots (rows without one are passed over), and the
+ * values that the slots hold back into rows (rows without one are left as they were).  What is loaded is exact in both types. */
+int iso_kv4_store(iso_ctx *ctx, const void *k, const void *v, const iso_kv4 *cache, const int *slots, int T, void *stream);
+int iso_kv4_load(iso_ctx *ctx, const iso_kv4 *cache, const int *slots, void *k, void *v, int T, void *stream);
+
+/* Attention of a batch of requests over their pages: single tokens, chunks of prompts, or both in one call.
+ *   q [total_rows, nq, d] (rows q_stride elements apart, a multiple of 8 and at least nq * d), out [total_rows, nq, d].
+ *   Request i has rows row_start[i] .. row_start[i+1]-1: the last tokens of its kv_len[i], whose keys and values are in the cache.
+ *   Row t of n sees key j iff j <= kv_len - n + t and the table has a page for j (an entry in [0, n_pages)); the rest as
+ *   iso_attn_chunk.  A row that sees no key is zero.  Rows in front of the first request or behind the last are left as they were;
+ *   what a cache holds in a token that a row does not see does not reach that row, NaN included.
+ *   max_rows: the most rows that one request has, as far as known; the kernels are chosen by it, results are right for any value >= 1.
+ *   ws: iso_attn_kv4_workspace bytes, zero-filled before its first use (every call leaves it ready for the next).  Calls that may
+ *   overlap in time, replays of a graph among them, need one each.
+ * Results do not depend on the order in which workgroups run.
+ * Errors: NULL, n_seqs outside [1, 4096], total_rows, max_rows or max_pages < 1, q_stride (ISO_ERR_SHAPE), ws too small
+ * (ISO_ERR_WORKSPACE). */
+int iso_attn_kv4_workspace(iso_ctx *ctx, int n_seqs, int total_rows, size_t *bytes);
+int iso_attn_kv4(iso_ctx *ctx, const void *q, int q_stride, const iso_kv4 *cache, const int *block_table, int max_pages,
+                 const int *row_start, const int *kv_len, int n_seqs, int total_rows, int max_rows, void *out, void *ws, size_t ws_bytes,
+                 void *stream);
+
 /* GEMM segmentation (Section 3.2, the remedy for the computation-dominated case): every projection of the layer
  * entry points is issued as n launches over consecutive row ranges (multiples of 256 rows; products with fewer
  * than 256 * n rows stay whole).  Results are the same bits as long as the segments take the same kernel variant
@@ -328,7 +396,7 @@ int iso_set_gemm_segments(iso_ctx *ctx, int n);
 typedef enum {
     ISO_K_GEMM_QKV = 0, ISO_K_GEMM_O = 1, ISO_K_GEMM_GATE_UP = 2, ISO_K_GEMM_DOWN = 3, ISO_K_ATTN = 4,
     ISO_K_RMSNORM = 5, ISO_K_RESID_NORM = 6, ISO_K_RESIDUAL = 7, ISO_K_ROPE_KV = 8, ISO_K_SWIGLU = 9,
-    ISO_K_COMM = 10, ISO_K_QUANT = 11, ISO_K_COUNT = 12
+    ISO_K_COMM = 10, ISO_K_QUANT = 11, ISO_K_TABLES = 12, ISO_K_COUNT = 13
 } iso_kernel_kind;
 int iso_timing_enable(iso_ctx *ctx, int on);
 int iso_timing_read(iso_ctx *ctx, int kind, double *total_ms, int *launches);

@@ -40,11 +40,12 @@ EXPORTS = [
     "iso_device_count", "iso_device_sync", "iso_dev_alloc", "iso_dev_free", "iso_dev_fill", "iso_host_alloc",
     "iso_host_free", "iso_copy_h2d", "iso_copy_d2h", "iso_copy_d2h_async", "iso_set_gemm_segments", "iso_quantize_rows_fp8", "iso_rmsnorm_fp8", "iso_gemm_fp8", "iso_gemm_launch_plan", "iso_copy_d2d", "iso_stream_create", "iso_stream_destroy",
     "iso_gemm_rowpar_static", "iso_streamk_status_word",
+    "iso_block_tables", "iso_rope_kv4_write", "iso_kv4_store", "iso_kv4_load", "iso_attn_kv4_workspace", "iso_attn_kv4",
 ]
 KERNEL_KINDS = ["gemm_qkv", "gemm_o", "gemm_gate_up", "gemm_down", "attn", "rmsnorm", "resid_norm", "residual",
-                "rope_kv", "swiglu", "comm", "quant"]
-DTYPE_BYTES = {"f32": 4, "bf16": 2, "u8": 1}
-_NP_STORAGE = {"f32": np.float32, "bf16": np.uint16, "u8": np.uint8}
+                "rope_kv", "swiglu", "comm", "quant", "tables"]
+DTYPE_BYTES = {"f32": 4, "bf16": 2, "u8": 1, "i32": 4}
+_NP_STORAGE = {"f32": np.float32, "bf16": np.uint16, "u8": np.uint8, "i32": np.int32}
 
 
 class IsoCfg(ctypes.Structure):
@@ -59,6 +60,11 @@ class IsoWeights(ctypes.Structure):
                 ("w_qkv_f8", ctypes.c_void_p), ("w_o_f8", ctypes.c_void_p), ("w_gate_up_f8", ctypes.c_void_p),
                 ("w_down_f8", ctypes.c_void_p), ("s_qkv", ctypes.c_void_p), ("s_o", ctypes.c_void_p),
                 ("s_gate_up", ctypes.c_void_p), ("s_down", ctypes.c_void_p)]
+
+
+class IsoKv4(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int), ("page", ctypes.c_int)]
 
 
 class IsoPlan(ctypes.Structure):
@@ -132,6 +138,13 @@ def load() -> ctypes.CDLL:
     lib.iso_quantize_rows_fp8.argtypes = [vp, vp, ci, ci, vp, vp, vp]
     lib.iso_rmsnorm_fp8.argtypes = [vp, vp, vp, vp, vp, vp, ci, vp]
     lib.iso_gemm_fp8.argtypes = [vp, vp, vp, vp, vp, vp, ci, ci, ci, vp]
+    pkv4 = ctypes.POINTER(IsoKv4)
+    lib.iso_block_tables.argtypes = [vp, vp, vp, ci, ci, vp, ci, vp, vp, ci, vp, vp, vp, vp, ci, vp, vp]
+    lib.iso_rope_kv4_write.argtypes = [vp, vp, vp, pkv4, vp, vp, ci, vp]
+    lib.iso_kv4_store.argtypes = [vp, vp, vp, pkv4, vp, ci, vp]
+    lib.iso_kv4_load.argtypes = [vp, pkv4, vp, vp, vp, ci, vp]
+    lib.iso_attn_kv4_workspace.argtypes = [vp, ci, ci, ctypes.POINTER(sz)]
+    lib.iso_attn_kv4.argtypes = [vp, vp, ci, pkv4, vp, ci, vp, vp, ci, ci, ci, vp, vp, sz, vp]
     lib.iso_copy_d2d.argtypes = [vp, vp, sz]
     lib.iso_stream_create.argtypes = [pvp]
     lib.iso_stream_destroy.argtypes = [vp]
@@ -350,6 +363,20 @@ def upload_weights(w: Dict[str, np.ndarray], dtype: str) -> Dict[str, DeviceArra
     return {k: DeviceArray.from_numpy(v, dtype) for k, v in w.items()}
 
 
+class Kv4Cache:
+    """A paged 4-bit key/value cache (iso_kv4).  Takes four device buffers of bytes, k and v [n_pages, nkv, page, d / 2], k_scale and
+    v_scale [n_pages, nkv, page, d / 32]; Context.kv4_cache allocates them."""
+
+    def __init__(self, page: int, k, v, k_scale, v_scale):
+        shapes = [tuple(int(n) for n in a.shape) for a in (k, v, k_scale, v_scale)]
+        if len(shapes[0]) != 4 or shapes[0] != shapes[1] or shapes[2] != shapes[3] or shapes[0][:3] != shapes[2][:3] or \
+                shapes[0][2] != page or shapes[2][3] * 16 != shapes[0][3]:
+            raise ValueError(f"not the buffers of a 4-bit cache with pages of {page} tokens: {shapes}")
+        self.page, self.n_pages, self.nkv, self.head_dim = page, shapes[0][0], shapes[0][1], 2 * shapes[0][3]
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale      # kept alive
+        self.handle = IsoKv4(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), self.n_pages, page)
+
+
 class Context:
     """Owns an iso_ctx.  `stream0`/`stream1`: Stream objects (created here if omitted)."""
 
@@ -485,3 +512,41 @@ class Context:
 
     def swiglu(self, gu, a, T: int, stream=None) -> None:
         _check(self._lib.iso_swiglu(self._h, _ptr(gu), _ptr(a), T, _stream_handle(stream)))
+
+    # ---- the paged 4-bit cache ------------------------------------------------------------------
+    def kv4_cache(self, n_pages: int, page: int = 64, fill_byte: Optional[int] = None) -> Kv4Cache:
+        nkv, d = self.cfg.n_kv_heads, self.cfg.head_dim
+        k, v = (DeviceArray((n_pages, nkv, page, d // 2), "u8", fill_byte) for _ in range(2))
+        ks, vs = (DeviceArray((n_pages, nkv, page, d // 32), "u8", fill_byte) for _ in range(2))
+        return Kv4Cache(page, k, v, ks, vs)
+
+    def _kv4(self, cache: Kv4Cache):
+        if (cache.nkv, cache.head_dim) != (self.cfg.n_kv_heads, self.cfg.head_dim):
+            raise ValueError(f"a cache of {cache.nkv} heads of {cache.head_dim}, the context has {self.cfg.n_kv_heads} of {self.cfg.head_dim}")
+        return ctypes.byref(cache.handle)
+
+    def block_tables(self, cached, fresh, n_seqs: int, page: int, free_pages, n_free: int, free_head, block_table, max_pages: int, row_start,
+                     kv_len, positions, slots, max_rows: int, free_next, stream=None) -> None:
+        _check(self._lib.iso_block_tables(self._h, _ptr(cached), _ptr(fresh), n_seqs, page, _ptr(free_pages), n_free, _ptr(free_head),
+                                          _ptr(block_table), max_pages, _ptr(row_start), _ptr(kv_len), _ptr(positions), _ptr(slots),
+                                          max_rows, _ptr(free_next), _stream_handle(stream)))
+
+    def rope_kv4_write(self, qkv, q_out, cache: Kv4Cache, positions, slots, T: int, stream=None) -> None:
+        _check(self._lib.iso_rope_kv4_write(self._h, _ptr(qkv), _ptr(q_out), self._kv4(cache), _ptr(positions), _ptr(slots), T,
+                                            _stream_handle(stream)))
+
+    def kv4_store(self, k, v, cache: Kv4Cache, slots, T: int, stream=None) -> None:
+        _check(self._lib.iso_kv4_store(self._h, _ptr(k), _ptr(v), self._kv4(cache), _ptr(slots), T, _stream_handle(stream)))
+
+    def kv4_load(self, cache: Kv4Cache, slots, k, v, T: int, stream=None) -> None:
+        _check(self._lib.iso_kv4_load(self._h, self._kv4(cache), _ptr(slots), _ptr(k), _ptr(v), T, _stream_handle(stream)))
+
+    def attn_kv4_workspace(self, n_seqs: int, total_rows: int) -> int:
+        n = ctypes.c_size_t()
+        _check(self._lib.iso_attn_kv4_workspace(self._h, n_seqs, total_rows, ctypes.byref(n)))
+        return n.value
+
+    def attn_kv4(self, q, q_stride: int, cache: Kv4Cache, block_table, max_pages: int, row_start, kv_len, n_seqs: int, total_rows: int,
+                 max_rows: int, out, ws, ws_bytes: int, stream=None) -> None:
+        _check(self._lib.iso_attn_kv4(self._h, _ptr(q), q_stride, self._kv4(cache), _ptr(block_table), max_pages, _ptr(row_start),
+                                      _ptr(kv_len), n_seqs, total_rows, max_rows, _ptr(out), _ptr(ws), ws_bytes, _stream_handle(stream)))

@@ -16,6 +16,7 @@
 #include <vector>
 
 #include "iso_internal.h"
+#include "kv4.h"
 
 namespace {
 
@@ -851,6 +852,29 @@ int run_split(iso_ctx *ctx, const iso_weights *layers, int n_layers, void *x, vo
     return run_stack(ctx, layers, n_layers, x, k_caches, v_caches, edges, two ? 2 : 1, comm, sched);
 }
 
+// ---- the paged 4-bit cache ---------------------------------------------------------------------
+bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+bool page_size_known(int page) { return page >= 16 && page <= 256 && (page & (page - 1)) == 0; }
+
+// The kernels run where the stream is, and the launch goes to the current device.
+int check_device(const iso_ctx *ctx) {
+    int dev = -1;
+    HIP_TRY(hipGetDevice(&dev));
+    if (dev != ctx->device) return fail(ISO_ERR_HIP, "device %d is current, the context is on device %d", dev, ctx->device);
+    return ISO_OK;
+}
+
+int check_kv4(const iso_kv4 *c) {
+    if (!c) return fail(ISO_ERR_NULL, "cache is NULL");
+    if (!c->k || !c->v || !c->k_scale || !c->v_scale) return fail(ISO_ERR_NULL, "the cache's k, v, k_scale and v_scale must be non-NULL");
+    if (!page_size_known(c->page)) return fail(ISO_ERR_SHAPE, "page=%d must be 16, 32, 64, 128 or 256", c->page);
+    if (c->n_pages < 1 || (long long)c->n_pages * c->page >= (1ll << 31))
+        return fail(ISO_ERR_SHAPE, "n_pages=%d of %d tokens: need at least one page and fewer than 2^31 tokens", c->n_pages, c->page);
+    if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->k_scale, 16) || !aligned(c->v_scale, 16))
+        return fail(ISO_ERR_SHAPE, "the cache's buffers must be 16-byte aligned");
+    return ISO_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1336,6 +1360,102 @@ int iso_swiglu(iso_ctx *ctx, const void *gu, void *a, int T, void *stream) {
     if (!gu || !a) return fail(ISO_ERR_NULL, "gu and a must be non-NULL");
     if (T < 1) return fail(ISO_ERR_SHAPE, "T=%d must be positive", T);
     LAUNCH_TRY(ISO_K_SWIGLU, (hipStream_t)stream, iso_launch_swiglu(ctx->cfg.dtype, gu, a, T, ctx->cfg.ffn, (hipStream_t)stream), "swiglu");
+    return ISO_OK;
+}
+
+int iso_block_tables(iso_ctx *ctx, const int *cached, const int *fresh, int n_seqs, int page, const int *free_pages, int n_free,
+                     const int *free_head, int *block_table, int max_pages, int *row_start, int *kv_len, int *positions, int *slots,
+                     int max_rows, int *free_next, void *stream) {
+    if (!ctx) return fail(ISO_ERR_NULL, "ctx is NULL");
+    if (!cached || !fresh || !block_table || !row_start || !kv_len || !positions || !slots || !free_next || (!free_pages && n_free > 0))
+        return fail(ISO_ERR_NULL, "lengths, free pages, tables and outputs must be non-NULL");
+    if (n_seqs < 1 || n_seqs > KV4_MAX_SEQS) return fail(ISO_ERR_SHAPE, "n_seqs=%d outside [1, %d]", n_seqs, KV4_MAX_SEQS);
+    if (!page_size_known(page)) return fail(ISO_ERR_SHAPE, "page=%d must be 16, 32, 64, 128 or 256", page);
+    if (n_free < 0 || max_pages < 1 || max_rows < 1)
+        return fail(ISO_ERR_SHAPE, "n_free=%d must be >= 0, max_pages=%d and max_rows=%d positive", n_free, max_pages, max_rows);
+    if (kv_len == cached || kv_len == fresh || free_next == free_head) return fail(ISO_ERR_SHAPE, "outputs must not be inputs");
+    const void *ints[] = {cached, fresh, free_pages, free_head, block_table, row_start, kv_len, positions, slots, free_next};
+    for (const void *p : ints)
+        if (!aligned(p, 4)) return fail(ISO_ERR_SHAPE, "int buffers must be 4-byte aligned");
+    ISO_TRY(check_device(ctx));
+    LAUNCH_TRY(ISO_K_TABLES, (hipStream_t)stream,
+               iso_launch_block_tables(cached, fresh, n_seqs, page, free_pages, n_free, free_head, block_table, max_pages, row_start, kv_len,
+                                       positions, slots, max_rows, free_next, (hipStream_t)stream), "block tables");
+    return ISO_OK;
+}
+
+int iso_rope_kv4_write(iso_ctx *ctx, void *qkv, void *q_out, const iso_kv4 *cache, const int *positions, const int *slots, int T,
+                       void *stream) {
+    if (!ctx) return fail(ISO_ERR_NULL, "ctx is NULL");
+    if (!qkv || !positions || !slots) return fail(ISO_ERR_NULL, "qkv, positions and slots must be non-NULL");
+    ISO_TRY(check_kv4(cache));
+    if (T < 1) return fail(ISO_ERR_SHAPE, "T=%d must be positive", T);
+    if (!aligned(qkv, 16) || !aligned(q_out, 16) || !aligned(positions, 4) || !aligned(slots, 4))
+        return fail(ISO_ERR_SHAPE, "qkv and q_out must be 16-byte aligned, positions and slots 4-byte");
+    ISO_TRY(check_device(ctx));
+    const iso_cfg &c = ctx->cfg;
+    LAUNCH_TRY(ISO_K_ROPE_KV, (hipStream_t)stream,
+               iso_launch_kv4_write(c.dtype, qkv, q_out, *cache, positions, slots, ctx->rope_cos, ctx->rope_sin, c.max_seq, T, c.n_q_heads,
+                                    c.n_kv_heads, c.head_dim, (hipStream_t)stream), "rope+kv4");
+    return ISO_OK;
+}
+
+int iso_kv4_store(iso_ctx *ctx, const void *k, const void *v, const iso_kv4 *cache, const int *slots, int T, void *stream) {
+    if (!ctx) return fail(ISO_ERR_NULL, "ctx is NULL");
+    if (!k || !v || !slots) return fail(ISO_ERR_NULL, "k, v and slots must be non-NULL");
+    ISO_TRY(check_kv4(cache));
+    if (T < 1) return fail(ISO_ERR_SHAPE, "T=%d must be positive", T);
+    if (!aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 4)) return fail(ISO_ERR_SHAPE, "k and v must be 16-byte aligned, slots 4-byte");
+    ISO_TRY(check_device(ctx));
+    const iso_cfg &c = ctx->cfg;
+    LAUNCH_TRY(ISO_K_QUANT, (hipStream_t)stream,
+               iso_launch_kv4_store(c.dtype, k, v, *cache, slots, T, c.n_kv_heads, c.head_dim, (hipStream_t)stream), "kv4 store");
+    return ISO_OK;
+}
+
+int iso_kv4_load(iso_ctx *ctx, const iso_kv4 *cache, const int *slots, void *k, void *v, int T, void *stream) {
+    if (!ctx) return fail(ISO_ERR_NULL, "ctx is NULL");
+    if (!k || !v || !slots) return fail(ISO_ERR_NULL, "k, v and slots must be non-NULL");
+    ISO_TRY(check_kv4(cache));
+    if (T < 1) return fail(ISO_ERR_SHAPE, "T=%d must be positive", T);
+    if (!aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 4)) return fail(ISO_ERR_SHAPE, "k and v must be 16-byte aligned, slots 4-byte");
+    ISO_TRY(check_device(ctx));
+    const iso_cfg &c = ctx->cfg;
+    LAUNCH_TRY(ISO_K_QUANT, (hipStream_t)stream,
+               iso_launch_kv4_load(c.dtype, *cache, slots, k, v, T, c.n_kv_heads, c.head_dim, (hipStream_t)stream), "kv4 load");
+    return ISO_OK;
+}
+
+int iso_attn_kv4_workspace(iso_ctx *ctx, int n_seqs, int total_rows, size_t *bytes) {
+    if (!ctx || !bytes) return fail(ISO_ERR_NULL, "ctx and bytes must be non-NULL");
+    if (n_seqs < 1 || n_seqs > KV4_MAX_SEQS) return fail(ISO_ERR_SHAPE, "n_seqs=%d outside [1, %d]", n_seqs, KV4_MAX_SEQS);
+    if (total_rows < 1) return fail(ISO_ERR_SHAPE, "total_rows=%d must be positive", total_rows);
+    *bytes = 256;
+    return ISO_OK;
+}
+
+int iso_attn_kv4(iso_ctx *ctx, const void *q, int q_stride, const iso_kv4 *cache, const int *block_table, int max_pages,
+                 const int *row_start, const int *kv_len, int n_seqs, int total_rows, int max_rows, void *out, void *ws, size_t ws_bytes,
+                 void *stream) {
+    if (!ctx) return fail(ISO_ERR_NULL, "ctx is NULL");
+    if (!q || !block_table || !row_start || !kv_len || !out || !ws)
+        return fail(ISO_ERR_NULL, "q, block_table, row_start, kv_len, out and ws must be non-NULL");
+    ISO_TRY(check_kv4(cache));
+    const iso_cfg &c = ctx->cfg;
+    if (max_rows < 1 || max_pages < 1) return fail(ISO_ERR_SHAPE, "max_rows=%d and max_pages=%d must be positive", max_rows, max_pages);
+    if (q_stride < c.n_q_heads * c.head_dim || q_stride % 8)
+        return fail(ISO_ERR_SHAPE, "q_stride=%d must be a multiple of 8, at least %d", q_stride, c.n_q_heads * c.head_dim);
+    size_t need = 0;
+    ISO_TRY(iso_attn_kv4_workspace(ctx, n_seqs, total_rows, &need));
+    if (ws_bytes < need) return fail(ISO_ERR_WORKSPACE, "ws of %zu bytes, %zu are needed", ws_bytes, need);
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(ws, 16) || !aligned(block_table, 4) || !aligned(row_start, 4) || !aligned(kv_len, 4))
+        return fail(ISO_ERR_SHAPE, "q, out and ws must be 16-byte aligned, int buffers 4-byte");
+    ISO_TRY(sk_status(ctx));
+    ISO_TRY(check_device(ctx));
+    const kv4_batch b{block_table, row_start, kv_len, max_pages, n_seqs, total_rows};
+    LAUNCH_TRY(ISO_K_ATTN, (hipStream_t)stream,
+               iso_launch_attn_kv4_simple(c.dtype, q, q_stride, *cache, b, out, c.n_q_heads, c.n_kv_heads, c.head_dim, (hipStream_t)stream),
+               "kv4 attention");
     return ISO_OK;
 }
 

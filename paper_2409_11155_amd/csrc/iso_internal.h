@@ -202,6 +202,20 @@ hipError_t iso_launch_attn_bf16_wave(const void *q, const void *k, const void *v
 size_t iso_attn_part_bytes(void);      // bytes of one partial state in an iso_attn_ws
 bool iso_attn_bf16_dtl_supported(int d, int kv_len, int nkv);
 
+// ---- the paged 4-bit cache (kv4.hip, attn_kv4*.hip)
+struct kv4_batch;
+hipError_t iso_launch_block_tables(const int *cached, const int *fresh, int n_seqs, int page, const int *free_pages, int n_free,
+                                   const int *free_head_or_null, int *table, int max_pages, int *row_start, int *kv_len, int *positions,
+                                   int *slots, int max_rows, int *free_next, hipStream_t s);
+hipError_t iso_launch_kv4_write(int dtype, void *qkv, void *q_out_or_null, const iso_kv4 &cache, const int *positions, const int *slots,
+                                const float *cos_t, const float *sin_t, int max_pos, int n_rows, int nq, int nkv, int d, hipStream_t s);
+hipError_t iso_launch_kv4_store(int dtype, const void *k_rows, const void *v_rows, const iso_kv4 &cache, const int *slots, int n_rows, int nkv,
+                                int d, hipStream_t s);
+hipError_t iso_launch_kv4_load(int dtype, const iso_kv4 &cache, const int *slots, void *k_rows, void *v_rows, int n_rows, int nkv, int d,
+                               hipStream_t s);
+hipError_t iso_launch_attn_kv4_simple(int dtype, const void *q, int q_stride, const iso_kv4 &cache, const kv4_batch &b, void *out, int nq,
+                                      int nkv, int d, hipStream_t s);
+
 // ---- small device helpers ----------------------------------------------------------------------
 __device__ __forceinline__ float iso_to_f32(float v) { return v; }
 __device__ __forceinline__ float iso_to_f32(bf16_t v) { return (float)v; }

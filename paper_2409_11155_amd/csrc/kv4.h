@@ -1,0 +1,43 @@
+// The 4-bit key/value cache: 32 neighbouring elements of a head (a block) share a scale 2^(byte - 127); an element is E2M1, a
+// sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (the OCP microscaling format with 4-bit elements).  A value has at most two
+// significant bits, so unpacking into bf16 rounds nothing.  Byte 255 is NaN for the whole block.
+#pragma once
+#include "iso_internal.h"
+
+constexpr int KV4_BLOCK = 32;
+constexpr int KV4_MAX_SEQS = 4096;      // requests in one call: their prefix sums are kept in LDS
+
+// Device view of an iso_kv4.  Strides in bytes; a page holds every kv head's tokens, a head's tokens are contiguous.
+struct kv4_view {
+    unsigned char *k, *v, *ks, *vs;
+    int n_pages, page, page_shift;
+};
+inline kv4_view kv4_view_of(const iso_kv4 &c) {
+    return kv4_view{(unsigned char *)c.k, (unsigned char *)c.v, (unsigned char *)c.k_scale, (unsigned char *)c.v_scale,
+                    c.n_pages, c.page, __builtin_ctz((unsigned)c.page)};
+}
+// Ragged batch: request i has rows [row_start[i], row_start[i+1]) of the step's tensors and kv_len[i] tokens, the rows' own among
+// them; token j is at offset j % page of page table[i * max_pages + j / page].
+struct kv4_batch {
+    const int *table, *row_start, *kv_len;
+    int max_pages, n_seqs, total_rows;
+};
+
+// Value of a scale byte, as the conversion instructions take it (they read the exponent field: 0 is 2^-127, 255 is NaN).
+__device__ __forceinline__ float kv4_scale(unsigned byte) { return __uint_as_float(byte << 23); }
+
+// Rows of request i that exist, and the position of its row t: base + t.
+struct kv4_rows {
+    int first, n, base;
+};
+__device__ __forceinline__ kv4_rows kv4_rows_of(const kv4_batch &b, int i) {
+    const int lo = b.row_start[i], hi = b.row_start[i + 1];
+    const int base = b.kv_len[i] - (hi - lo);
+    const int first = max(0, lo), last = min(b.total_rows, hi);
+    return kv4_rows{first, max(0, last - first), base + (first - lo)};
+}
+// Keys of request i that its table can hold.
+__device__ __forceinline__ int kv4_keys_of(const kv4_batch &b, int i, int page_shift) {
+    const long long cap = (long long)b.max_pages << page_shift;
+    return (int)min((long long)max(0, b.kv_len[i]), cap);
+}
