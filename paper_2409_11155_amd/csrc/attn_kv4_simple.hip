@@ -19,14 +19,14 @@ __global__ __launch_bounds__(256) void attn_kv4_simple_kernel(const T *__restric
         else hi = mid;
         i = lo;
     }
-    const kv4_rows rw = kv4_rows_of(b, i);
+    const kv4_rows rw = kv4_rows_of(b.row_start, b.kv_len, b.total_rows, i);
     const bool active = row >= rw.first && row < rw.first + rw.n;
     const float scale = 1.0f / sqrtf((float)D);
     if (active)
         for (int e = lane; e < D; e += 64) qs[wave][e] = iso_to_f32(q[(size_t)row * q_stride + (size_t)h * D + e]) * scale;
     __syncthreads();
     if (!active) return;                                // rows in front of the first request or behind the last
-    const int keys = kv4_keys_of(b, i, c.page_shift);
+    const int keys = kv4_keys_of(b.kv_len, b.max_pages, i, c.page_shift);
     const int n_vis = min(keys, rw.base + (row - rw.first) + 1);
     const int *table = b.table + (size_t)i * b.max_pages;
     float o[PER] = {};

@@ -1430,7 +1430,9 @@ int iso_attn_kv4_workspace(iso_ctx *ctx, int n_seqs, int total_rows, size_t *byt
     if (!ctx || !bytes) return fail(ISO_ERR_NULL, "ctx and bytes must be non-NULL");
     if (n_seqs < 1 || n_seqs > KV4_MAX_SEQS) return fail(ISO_ERR_SHAPE, "n_seqs=%d outside [1, %d]", n_seqs, KV4_MAX_SEQS);
     if (total_rows < 1) return fail(ISO_ERR_SHAPE, "total_rows=%d must be positive", total_rows);
-    *bytes = 256;
+    if ((long long)total_rows * ctx->cfg.n_q_heads >= (1ll << 31))
+        return fail(ISO_ERR_SHAPE, "total_rows=%d of %d heads: fewer than 2^31 together", total_rows, ctx->cfg.n_q_heads);
+    *bytes = iso_attn_kv4_few_ws_bytes(ctx->cfg.head_dim, iso_num_cu());
     return ISO_OK;
 }
 
@@ -1453,9 +1455,13 @@ int iso_attn_kv4(iso_ctx *ctx, const void *q, int q_stride, const iso_kv4 *cache
     ISO_TRY(sk_status(ctx));
     ISO_TRY(check_device(ctx));
     const kv4_batch b{block_table, row_start, kv_len, max_pages, n_seqs, total_rows};
-    LAUNCH_TRY(ISO_K_ATTN, (hipStream_t)stream,
-               iso_launch_attn_kv4_simple(c.dtype, q, q_stride, *cache, b, out, c.n_q_heads, c.n_kv_heads, c.head_dim, (hipStream_t)stream),
-               "kv4 attention");
+    const hipStream_t s = (hipStream_t)stream;
+    if (ctx->flags & ISO_FLAG_SIMPLE_ATTN)
+        LAUNCH_TRY(ISO_K_ATTN, s, iso_launch_attn_kv4_simple(c.dtype, q, q_stride, *cache, b, out, c.n_q_heads, c.n_kv_heads, c.head_dim, s),
+                   "kv4 attention");
+    else
+        LAUNCH_TRY(ISO_K_ATTN, s, iso_launch_attn_kv4_few(c.dtype, q, q_stride, *cache, b, 0x7fffffff, out, c.n_q_heads, c.n_kv_heads,
+                                                          c.head_dim, ws, s), "kv4 attention");
     return ISO_OK;
 }
 

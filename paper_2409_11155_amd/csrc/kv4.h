@@ -30,14 +30,14 @@ __device__ __forceinline__ float kv4_scale(unsigned byte) { return __uint_as_flo
 struct kv4_rows {
     int first, n, base;
 };
-__device__ __forceinline__ kv4_rows kv4_rows_of(const kv4_batch &b, int i) {
-    const int lo = b.row_start[i], hi = b.row_start[i + 1];
-    const int base = b.kv_len[i] - (hi - lo);
-    const int first = max(0, lo), last = min(b.total_rows, hi);
+template <typename P> __device__ __forceinline__ kv4_rows kv4_rows_of(P row_start, P kv_len, int total_rows, int i) {
+    const int lo = row_start[i], hi = row_start[i + 1];
+    const int base = kv_len[i] - (hi - lo);
+    const int first = max(0, lo), last = min(total_rows, hi);
     return kv4_rows{first, max(0, last - first), base + (first - lo)};
 }
 // Keys of request i that its table can hold.
-__device__ __forceinline__ int kv4_keys_of(const kv4_batch &b, int i, int page_shift) {
-    const long long cap = (long long)b.max_pages << page_shift;
-    return (int)min((long long)max(0, b.kv_len[i]), cap);
+template <typename P> __device__ __forceinline__ int kv4_keys_of(P kv_len, int max_pages, int i, int page_shift) {
+    const long long cap = (long long)max_pages << page_shift;
+    return (int)min((long long)max(0, kv_len[i]), cap);
 }
