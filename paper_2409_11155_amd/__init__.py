@@ -328,11 +328,12 @@ class Stream:
 
 
 def _ptr(t) -> Optional[int]:
-    if t is None:
-        return None
-    if isinstance(t, int):
+    if type(t) is DeviceArray:
+        return t.ptr
+    if t is None or isinstance(t, int):
         return t
-    if hasattr(t, "is_contiguous") and not t.is_contiguous():
+    contiguous = getattr(t, "is_contiguous", None)
+    if contiguous is not None and not contiguous():
         raise ValueError("libiso takes contiguous buffers")
     return t.data_ptr()
 

@@ -21,10 +21,14 @@
 namespace {
 
 constexpr int WAVES = 4, THREADS = 64 * WAVES, TILE = 32, UNIT = WAVES * TILE, ROWS = 16;
+constexpr int FOLD = 128, SPLITS = FOLD - 2;              // pieces of a triple, at most (two less than the fold takes: a share may start and end inside one)
 constexpr int COHERENT = 1 | 16;         // buffer cache policy sc0 | sc1: system scope, bypasses the XCD-local L2
 
 typedef __bf16 bf16x4_v __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2_v __attribute__((ext_vector_type(2)));
 
+// Workgroups on a compute unit, by the registers: float keeps three terms of q.
+constexpr int wg_per_cu(int elt, int d) { return elt == 4 ? (d == 64 ? 3 : 2) : d == 64 ? 4 : 3; }
 template <int D> constexpr int slot_floats() { return ROWS * (D + 2); }      // output rows, then maxima, then sums
 
 struct few_args {
@@ -66,18 +70,34 @@ __device__ __forceinline__ bf16x8_t unpack8(unsigned w, float scale) {
 // Wave-uniform values are made scalar explicitly, and what is read at a uniform place is read by the scalar unit: vector loads come
 // back in order, so a page number among them would have to wait for the codes requested before it.
 typedef const __attribute__((address_space(4))) int *scalar_ints;
+// Buffer over the 4 GB from p + (at & ~0xffffffff) on: with the low half of `at` as the scalar offset, a lane's address is p + at + its own
+// offset without an addition in a vector register.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t beyond(unsigned char *p, uint64_t at) {
+    return __builtin_amdgcn_make_buffer_rsrc((void *)(p + (at & 0xffffffff00000000ull)), 0, -1, 0x00020000);
+}
 __device__ __forceinline__ scalar_ints scalar(const int *p) { return (scalar_ints)(uintptr_t)p; }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ unsigned uniform(unsigned x) { return (unsigned)__builtin_amdgcn_readfirstlane((int)x); }
 
+// Inclusive sum and maximum over the wave, lane 63 holds all of it: row shifts, then the last lanes of the rows handed on (DPP, no LDS).
+template <typename F> __device__ __forceinline__ unsigned wave_scan(unsigned x, F f) {
+    x = f(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false));
+    x = f(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false));
+    x = f(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false));
+    x = f(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false));
+    x = f(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));
+    x = f(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));
+    return x;
+}
+
 template <typename T, int D>
-__global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 2 : 3) void attn_kv4_few_kernel(few_args a) {
+__global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D)) void attn_kv4_few_kernel(few_args a) {
     constexpr int NP = sizeof(T) == 4 ? 3 : 1;
     constexpr int WPL = D / 32;              // code words (8 elements) a lane takes of a key
     constexpr int RB = 2 * D;                // bytes of an unpacked row
+    constexpr int VG = D == 64 ? 2 : 1;      // blocks of 16 dims of V that are read at a time
     __shared__ __attribute__((aligned(1024))) unsigned char lds[WAVES * TILE * RB];
     __shared__ float ml[2][WAVES][ROWS];
-    __shared__ unsigned wave_sum[WAVES], wave_max[WAVES], found, found_at;
     __shared__ int last_arriver;
 
     const int tid = threadIdx.x, lane = tid & 63, n16 = lane & 15, g4 = lane >> 4;
@@ -95,59 +115,42 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 2 : 3) void attn_kv4_few_
         q.units = max(1u, ((unsigned)q.keys + unit - 1) >> a.unit_shift);
         return q;
     };
-    const int per_thread = (b.n_seqs + THREADS - 1) / THREADS;
-    const int i_lo = min(b.n_seqs, tid * per_thread), i_hi = min(b.n_seqs, i_lo + per_thread);
+    // Every wave does this for itself, 64 requests at a time: no barrier, and for up to 64 of them one trip to memory.
+    auto add = [](unsigned x, unsigned y) { return x + y; };
     unsigned mine = 0, longest = 0;
-    for (int i = i_lo; i < i_hi; ++i) {
-        const Req q = request(i);
-        mine += q.tiles * q.units;
-        if (q.tiles) longest = max(longest, q.units);
+    for (int i0 = 0; i0 < b.n_seqs; i0 += 64) {
+        const Req q = request(min(i0 + lane, b.n_seqs - 1));
+        const unsigned u = i0 + lane < b.n_seqs ? q.tiles * q.units : 0;
+        mine += u;
+        if (u) longest = max(longest, q.units);
     }
-    unsigned incl = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const unsigned x = __shfl_up(incl, o, 64);
-        if (lane >= o) incl += x;
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) longest = max(longest, (unsigned)__shfl_xor(longest, o, 64));
-    if (lane == 63) wave_sum[wave] = incl;
-    if (lane == 0) wave_max[wave] = longest;
-    __syncthreads();
-    unsigned before = incl - mine, all = 0;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-        if (w < wave) before += wave_sum[w];
-        all += wave_sum[w];
-        longest = max(longest, wave_max[w]);
-    }
-    all = uniform(all);
-    longest = uniform(longest);
+    unsigned incl = wave_scan(mine, add);
+    const unsigned all = (unsigned)__builtin_amdgcn_readlane((int)incl, 63);
+    longest = (unsigned)__builtin_amdgcn_readlane((int)wave_scan(longest, [](unsigned x, unsigned y) { return max(x, y); }), 63);
     if (all == 0) return;
     const unsigned total = all * (unsigned)a.nkv;
-    const unsigned per = uniform(max((total + a.wgs - 1) / a.wgs, (longest + 63) / 64));
+    const unsigned per = uniform(max((total + a.wgs - 1) / a.wgs, (longest + SPLITS - 1) / SPLITS));
     unsigned at = blockIdx.x * per;
     const unsigned end = min(total, at + per);
     if (at >= end) return;
     // ---- the request that holds the first unit
-    int kvh = (int)uniform(at / all);
-    const unsigned in_head = at - (unsigned)kvh * all;
-    if (in_head >= before && in_head < before + mine) {
-        unsigned x = before;
-        for (int i = i_lo; i < i_hi; ++i) {
-            const Req q = request(i);
-            const unsigned u = q.tiles * q.units;
-            if (in_head < x + u) {
-                found = i;
-                found_at = in_head - x;
-                break;
-            }
-            x += u;
+    int kvh = (int)uniform(at / all), seq = 0;
+    unsigned inside = at - (unsigned)kvh * all;
+    for (int i0 = 0;; i0 += 64) {
+        if (b.n_seqs > 64) {
+            const Req q = request(min(i0 + lane, b.n_seqs - 1));
+            mine = i0 + lane < b.n_seqs ? q.tiles * q.units : 0;
+            incl = wave_scan(mine, add);
         }
+        const uint64_t in_front = __builtin_amdgcn_ballot_w64(incl <= inside);      // requests that end before it
+        const int n = __builtin_popcountll(in_front);
+        if (n < 64) {
+            seq = i0 + n;
+            inside -= n ? (unsigned)__builtin_amdgcn_readlane((int)incl, n - 1) : 0u;
+            break;
+        }
+        inside -= (unsigned)__builtin_amdgcn_readlane((int)incl, 63);
     }
-    __syncthreads();
-    int seq = uniform((int)found);
-    unsigned inside = uniform(found_at);
 
     const float sc = 1.4426950408889634f / sqrtf((float)D);
     const unsigned lds_w = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds + wave * TILE * RB;
@@ -155,6 +158,7 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 2 : 3) void attn_kv4_few_
     // V: the lane's row on the way in is n16 (+ 16), on the way out 4 g4 + n16 / 4 (+ 16)
     unsigned char *const v_in = lds + wave * TILE * RB + n16 * RB;
     const int in_swz = swz(n16);
+    const unsigned code_at = n16 * (D / 2) + g4 * WPL * 4, scale_at = n16 * (D / KV4_BLOCK) + g4 * WPL / 4;
     const int out_row = 4 * g4 + (n16 >> 2);
     const unsigned v_out = lds_w + out_row * RB + ((((n16 & 3) >> 1) ^ swz(out_row)) << 4) + ((n16 & 1) << 3);
 
@@ -191,44 +195,40 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 2 : 3) void attn_kv4_few_
         float m_run = -INFINITY, l_run = 0.f;          // maximum in units of the base-2 exponent
 
         const scalar_ints table = scalar(b.table + (size_t)seq * b.max_pages);
+        int k0 = (int)min((long long)ua << a.unit_shift, (long long)lim_hi) + wave * TILE;
+        const int k_end = (int)min((long long)ub << a.unit_shift, (long long)lim_hi);
         struct Pages { int p[2]; };
         auto pages_of = [&](int k0) {
             Pages x;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) x.p[h] = k0 + 16 * h < lim_hi ? table[(k0 + 16 * h) >> shift] : -1;
+            for (int h = 0; h < 2; ++h) x.p[h] = k0 + 16 * h < k_end ? table[(k0 + 16 * h) >> shift] : -1;
             return x;
         };
         struct Codes { unsigned k[2][WPL], v[2][WPL]; unsigned ks[2], vs[2]; int there; };
-        // Codes and scales of the wave's 32 keys from k0 on; what no row sees, and pages that do not exist, read as zero.
+        // Codes and scales of the wave's 32 keys from k0 on.  Where there is no page the first one is read instead, and what lies behind the
+        // last visible key is read too: multiply() leaves both out.
         auto fetch = [&](int k0, const Pages &pages, Codes &c) {
             c.there = 0;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int key = k0 + 16 * h;
-                const int page = pages.p[h];
-                const bool there = page >= 0 && page < a.c.n_pages;
+                const bool there = (unsigned)pages.p[h] < (unsigned)a.c.n_pages;
                 c.there |= (int)there << h;
-                const int first = key & ~(a.c.page - 1);                       // the page's first key
-                const int toks = there ? min(a.c.page, lim_hi - first) : 0;
-                const size_t tok = (((size_t)(there ? page : 0) * a.nkv + kvh) << shift);
-                const unsigned off = (unsigned)(key - first + n16);
-                const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc((void *)(a.c.k + tok * (D / 2)), 0, toks * (D / 2), 0x00020000);
-                const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void *)(a.c.v + tok * (D / 2)), 0, toks * (D / 2), 0x00020000);
-                const __amdgpu_buffer_rsrc_t rks = __builtin_amdgcn_make_buffer_rsrc((void *)(a.c.ks + tok * (D / 32)), 0, toks * (D / 32), 0x00020000);
-                const __amdgpu_buffer_rsrc_t rvs = __builtin_amdgcn_make_buffer_rsrc((void *)(a.c.vs + tok * (D / 32)), 0, toks * (D / 32), 0x00020000);
-                const unsigned ob = off * (D / 2) + g4 * WPL * 4, os = off * (D / 32) + (D == 128 ? g4 : g4 >> 1);
+                const uint64_t tok = (((uint64_t)(unsigned)(there ? pages.p[h] : 0) * (unsigned)a.nkv + (unsigned)kvh) << shift) + ((k0 + 16 * h) & (a.c.page - 1));
+                const uint64_t at_c = tok * (D / 2), at_s = tok * (D / KV4_BLOCK);
+                const auto rk = beyond(a.c.k, at_c), rv = beyond(a.c.v, at_c), rks = beyond(a.c.ks, at_s), rvs = beyond(a.c.vs, at_s);
                 if constexpr (D == 128) {
-                    const u32x4_t x = __builtin_amdgcn_raw_buffer_load_b128(rk, ob, 0, 0), y = __builtin_amdgcn_raw_buffer_load_b128(rv, ob, 0, 0);
+                    const u32x4_t x = __builtin_amdgcn_raw_buffer_load_b128(rk, code_at, (unsigned)at_c, 0);
+                    const u32x4_t y = __builtin_amdgcn_raw_buffer_load_b128(rv, code_at, (unsigned)at_c, 0);
 #pragma unroll
                     for (int w = 0; w < WPL; ++w) c.k[h][w] = x[w], c.v[h][w] = y[w];
                 } else {
-                    typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
-                    const u32x2_t x = __builtin_amdgcn_raw_buffer_load_b64(rk, ob, 0, 0), y = __builtin_amdgcn_raw_buffer_load_b64(rv, ob, 0, 0);
+                    const u32x2_v x = __builtin_amdgcn_raw_buffer_load_b64(rk, code_at, (unsigned)at_c, 0);
+                    const u32x2_v y = __builtin_amdgcn_raw_buffer_load_b64(rv, code_at, (unsigned)at_c, 0);
 #pragma unroll
                     for (int w = 0; w < WPL; ++w) c.k[h][w] = x[w], c.v[h][w] = y[w];
                 }
-                c.ks[h] = __builtin_amdgcn_raw_buffer_load_b8(rks, os, 0, 0);
-                c.vs[h] = __builtin_amdgcn_raw_buffer_load_b8(rvs, os, 0, 0);
+                c.ks[h] = __builtin_amdgcn_raw_buffer_load_b8(rks, scale_at, (unsigned)at_s, 0);
+                c.vs[h] = __builtin_amdgcn_raw_buffer_load_b8(rvs, scale_at, (unsigned)at_s, 0);
             }
         };
         auto multiply = [&](int k0, Codes &c) {
@@ -238,8 +238,9 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 2 : 3) void attn_kv4_few_
             if (masked) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    nan_v[h] = __builtin_amdgcn_ballot_w64(c.vs[h] == 255);
-                    if (c.vs[h] == 255) {
+                    const bool seen = (c.there >> h & 1) && k0 + 16 * h + n16 < lim_hi;
+                    nan_v[h] = __builtin_amdgcn_ballot_w64(seen && c.vs[h] == 255);
+                    if (!seen || c.vs[h] == 255) {
                         c.vs[h] = 127;
 #pragma unroll
                         for (int w = 0; w < WPL; ++w) c.v[h][w] = 0;
@@ -265,6 +266,17 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 2 : 3) void attn_kv4_few_
                 for (int w = 0; w < WPL; ++w)
                     *reinterpret_cast<bf16x8_t *>(v_in + h * 16 * RB + (((g4 * WPL + w) ^ in_swz) << 4)) = unpack8(c.v[h][w], f);
             }
+            // V comes back VG blocks of 16 dims at a time: the first ones while the probabilities are computed, then one group ahead
+            bf16x8_t vf[2][VG];
+            auto read_v = [&](int buf, int dt0) {
+#pragma unroll
+                for (int i = 0; i < VG; ++i) {
+                    const unsigned at = v_out ^ (unsigned)((dt0 + i) << 5);
+                    vf[buf][i] = __builtin_shufflevector(read_tr(at), read_tr(at + 16 * RB), 0, 1, 2, 3, 4, 5, 6, 7);
+                }
+            };
+            read_v(0, 0);
+            __builtin_amdgcn_sched_barrier(0);
             if (masked) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
@@ -303,36 +315,45 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 2 : 3) void attn_kv4_few_
                     for (int x = 0; x < NP; ++x) pb[x][4 * h + e] = part[x];
                 }
 #pragma unroll
-            for (int dt = 0; dt < D / 16; ++dt) {
-                const bf16x8_t vf = __builtin_shufflevector(read_tr((v_out ^ (dt << 5))), read_tr((v_out ^ (dt << 5)) + 16 * RB), 0, 1, 2, 3, 4, 5, 6, 7);
+            for (int grp = 0; grp < D / 16 / VG; ++grp) {
+                if (grp + 1 < D / 16 / VG) read_v((grp + 1) & 1, VG * (grp + 1));
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int p = 0; p < NP; ++p) o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb[p], o[dt], 0, 0, 0);
+                for (int i = 0; i < VG; ++i)
+#pragma unroll
+                    for (int p = 0; p < NP; ++p)
+                        o[VG * grp + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[grp & 1][i], pb[p], o[VG * grp + i], 0, 0, 0);
             }
             // a token whose V is NaN in some block: so is that block of the rows that see it, and of no others
+            if ((nan_v[0] | nan_v[1]) != 0) {
+                unsigned blocks = 0;                       // bit = 16 dims
+                for (int h = 0; h < 2; ++h)
+                    for (uint64_t m = h ? nan_v[1] : nan_v[0]; m; m &= m - 1) {
+                        const int bit = __builtin_ctzll(m);
+                        if (k0 + 16 * h + (bit & 15) < lim) blocks |= ((1u << D / 64) - 1) << (bit >> 4) * (D / 64);
+                    }
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                for (uint64_t m = nan_v[h]; m; m &= m - 1) {
-                    const int bit = __builtin_ctzll(m), key = k0 + 16 * h + (bit & 15), quarter = bit >> 4;
-#pragma unroll
-                    for (int dt = 0; dt < D / 16; ++dt)
-                        if (dt * 4 / (D / 16) == quarter && key < lim) o[dt] = f32x4_t{NAN, NAN, NAN, NAN};
-                }
+                for (int dt = 0; dt < D / 16; ++dt)
+                    if (blocks >> dt & 1) o[dt] = f32x4_t{NAN, NAN, NAN, NAN};
+            }
         };
 
         {
-            Codes now, next;
-            int k0 = (int)min((long long)ua << a.unit_shift, (long long)lim_hi) + wave * TILE;
-            const int k_end = (int)min((long long)ub << a.unit_shift, (long long)lim_hi);
-            Pages pages = pages_of(k0);
-            if (k0 < k_end) fetch(k0, pages, now);
-            pages = pages_of(k0 + UNIT);
-            while (k0 < k_end) {
-                const int k1 = k0 + UNIT;
-                if (k1 < k_end) fetch(k1, pages, next);
-                pages = pages_of(k1 + UNIT);
+            // Codes are requested a tile ahead and page numbers two, without a branch: behind the share's end there are no pages,
+            // and what has none is not fetched.  (A branch around the requests would make every wait one for all of them.)
+            Codes c0, c1;
+            fetch(k0, pages_of(k0), c0);
+            Pages pages = pages_of(k0 + UNIT);
+            auto step = [&](Codes &now, Codes &later) {
+                fetch(k0 + UNIT, pages, later);
+                pages = pages_of(k0 + 2 * UNIT);
                 multiply(k0, now);
-                now = next;
-                k0 = k1;
+                k0 += UNIT;
+            };
+            while (k0 < k_end) {
+                step(c0, c1);
+                if (k0 >= k_end) break;
+                step(c1, c0);
             }
         }
         // ---- the four waves' states
@@ -388,26 +409,63 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 2 : 3) void attn_kv4_few_
             }
             __syncthreads();
             writes = last_arriver != 0;
-            if (writes && real_row) {
-                m = -INFINITY;
-                l = 0.f;
+            if (writes) {
+                // All maxima and sums at once, then the rows with their weights.  Sixteen threads take a row of a piece; where the tile
+                // has fewer than 16 rows, the threads left over take every second (fourth, ...) piece.
+                const int n = w1 - w0 + 1, frow = tid & 15;
+                float mw[FOLD / 16], lw[FOLD / 16], top = -INFINITY, lsum = 0.f;
+#pragma unroll
+                for (int k = 0; k < FOLD / 16; ++k) {
+                    const int w = (tid >> 4) + 16 * k;
+                    mw[k] = -INFINITY;
+                    lw[k] = 0.f;
+                    if (w < n && (int)tile * ROWS + frow < pairs) {
+                        mw[k] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rp, slot(w0 + w) + (ROWS * D + frow) * 4, 0, COHERENT));
+                        lw[k] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rp, slot(w0 + w) + (ROWS * D + ROWS + frow) * 4, 0, COHERENT));
+                    }
+                }
+                float *const wt = reinterpret_cast<float *>(lds), *const red = wt + FOLD * ROWS;      // weights [piece][row]; [16][16]
+#pragma unroll
+                for (int k = 0; k < FOLD / 16; ++k) top = fmaxf(top, mw[k]);
+                red[tid] = top;
+                __syncthreads();
+#pragma unroll
+                for (int k = 0; k < 16; ++k) top = fmaxf(top, red[16 * k + frow]);
+#pragma unroll
+                for (int k = 0; k < FOLD / 16; ++k) {
+                    const float f = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mw[k] - top);
+                    lsum += lw[k] * f;
+                    wt[tid + 256 * k] = f;
+                }
+                __syncthreads();
+                red[tid] = lsum;
+                __syncthreads();
+                const int rows = min(ROWS, pairs - (int)tile * ROWS), rs = rows > 8 ? 4 : rows > 4 ? 3 : rows > 2 ? 2 : rows > 1 ? 1 : 0;
+                const int my_row = (tid >> 4) & ((1 << rs) - 1), part = tid >> (4 + rs), parts = 16 >> rs;
 #pragma unroll
                 for (int x = 0; x < CPT; ++x) sum[x] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-                for (int w = w0; w <= w1; ++w) {
-                    const unsigned p = slot(w);
-                    f32x4_t v[CPT];
+                if (my_row < rows) {
+#pragma unroll 8
+                    for (int w = part; w < n; w += parts) {
+                        const float f = wt[w * ROWS + my_row];
 #pragma unroll
-                    for (int x = 0; x < CPT; ++x)
-                        v[x] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rp, p + (row * D + (col * CPT + x) * 4) * 4, 0, COHERENT));
-                    const float mw = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rp, p + (ROWS * D + row) * 4, 0, COHERENT));
-                    const float lw = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rp, p + (ROWS * D + ROWS + row) * 4, 0, COHERENT));
-                    const float m_new = fmaxf(m, mw);
-                    const float fa = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
-                    const float fb = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mw - m_new);
-                    m = m_new;
-                    l = l * fa + lw * fb;
+                        for (int x = 0; x < CPT; ++x)
+                            sum[x] += f * __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rp, slot(w0 + w) + (my_row * D + (col * CPT + x) * 4) * 4, 0, COHERENT));
+                    }
+                }
+                l = 0.f;
 #pragma unroll
-                    for (int x = 0; x < CPT; ++x) sum[x] = sum[x] * fa + v[x] * fb;
+                for (int k = 0; k < 16; ++k) l += red[16 * k + row];
+                __syncthreads();
+                f32x4_t *const rest = reinterpret_cast<f32x4_t *>(lds);        // [part][row][16 * CPT], over the weights
+#pragma unroll
+                for (int x = 0; x < CPT; ++x) rest[(tid >> 4) * 16 * CPT + col * CPT + x] = sum[x];
+                __syncthreads();
+#pragma unroll
+                for (int x = 0; x < CPT; ++x) {
+                    sum[x] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                    if (real_row)
+                        for (int k = 0; k < parts; ++k) sum[x] += rest[((k << rs) + row) * 16 * CPT + col * CPT + x];
                 }
             }
         }
@@ -440,10 +498,10 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 2 : 3) void attn_kv4_few_
 
 // Workgroups of the line, at most: as many as the chip holds at once.
 namespace {
-int few_wgs(int ncu) { return 3 * min(ncu, 512); }
+int few_wgs(int ncu, int elt, int d) { return wg_per_cu(elt, d) * min(ncu, 512); }
 size_t few_bytes(int d, int wgs) { return (size_t)wgs * 4 + (size_t)2 * wgs * (d == 64 ? slot_floats<64>() : slot_floats<128>()) * 4; }
 }  // namespace
-size_t iso_attn_kv4_few_ws_bytes(int d, int ncu) { return few_bytes(d, few_wgs(ncu)) + 256; }
+size_t iso_attn_kv4_few_ws_bytes(int d, int ncu) { return few_bytes(d, few_wgs(ncu, 2, d)) + 256; }
 
 hipError_t iso_launch_attn_kv4_few(int dtype, const void *q, int q_stride, const iso_kv4 &cache, const kv4_batch &b, int most, void *out,
                                    int nq, int nkv, int d, void *ws, hipStream_t s) {
@@ -453,9 +511,9 @@ hipError_t iso_launch_attn_kv4_few(int dtype, const void *q, int q_stride, const
     auto units = [&]() { return tiles * ((keys + (1ll << shift) - 1) >> shift); };
     while (units() >= (1ll << 31) && shift < 30) ++shift;
     if (units() >= (1ll << 31)) return hipErrorInvalidValue;
-    const int wgs = (int)min((long long)few_wgs(iso_num_cu()), units());    // no more workgroups than units
+    const int wgs = (int)min((long long)few_wgs(iso_num_cu(), dtype == ISO_F32 ? 4 : 2, d), units());    // no more workgroups than units
     few_args a{q, out, nullptr, (unsigned *)ws, kv4_view_of(cache), b, q_stride, nq, nkv, nq / nkv, wgs, most, shift};
-    a.part = (float *)((char *)ws + (((size_t)few_wgs(iso_num_cu()) * 4 + 255) & ~(size_t)255));
+    a.part = (float *)((char *)ws + (((size_t)few_wgs(iso_num_cu(), dtype == ISO_F32 ? 4 : 2, d) * 4 + 255) & ~(size_t)255));
     if (dtype == ISO_F32 && d == 64) hipLaunchKernelGGL((attn_kv4_few_kernel<float, 64>), dim3(wgs), dim3(THREADS), 0, s, a);
     else if (dtype == ISO_F32 && d == 128) hipLaunchKernelGGL((attn_kv4_few_kernel<float, 128>), dim3(wgs), dim3(THREADS), 0, s, a);
     else if (dtype == ISO_BF16 && d == 64) hipLaunchKernelGGL((attn_kv4_few_kernel<bf16_t, 64>), dim3(wgs), dim3(THREADS), 0, s, a);

@@ -219,6 +219,10 @@ size_t iso_attn_kv4_few_ws_bytes(int d, int ncu);
 // requests of at most `most` (row, query head of a key head) pairs
 hipError_t iso_launch_attn_kv4_few(int dtype, const void *q, int q_stride, const iso_kv4 &cache, const kv4_batch &b, int most, void *out,
                                    int nq, int nkv, int d, void *ws, hipStream_t s);
+// bf16, requests of more than `most` pairs, at most 64 query heads of a key head
+size_t iso_attn_kv4_rows_ws_bytes(int nkv, int d, int ncu);
+hipError_t iso_launch_attn_kv4_rows(const void *q, int q_stride, const iso_kv4 &cache, const kv4_batch &b, int most, void *out, int nq, int nkv,
+                                    int d, void *ws, hipStream_t s);
 
 // ---- small device helpers ----------------------------------------------------------------------
 __device__ __forceinline__ float iso_to_f32(float v) { return v; }
