@@ -875,24 +875,6 @@ int check_kv4(const iso_kv4 *c) {
     return ISO_OK;
 }
 
-// Which kernels a batch needs, and the bytes of workspace that each has (a call's workspace holds both regions whatever max_rows says).
-constexpr int KV4_FEW = 64;      // (row, query head of a key head) pairs of a request up to which it belongs to the kernel for few rows
-struct Kv4Launch {
-    bool few, rows;
-    size_t few_bytes, rows_bytes;
-};
-Kv4Launch kv4_launch(const iso_cfg &c, int n_seqs, int total_rows, int max_rows) {
-    const int G = c.n_q_heads / c.n_kv_heads, ncu = iso_num_cu();
-    const bool can = c.dtype == ISO_BF16 && G <= 64;
-    auto many = [&](int rows) { return can && (long long)rows * G > KV4_FEW; };
-    Kv4Launch l;
-    l.rows = many(n_seqs == 1 ? total_rows : std::min(max_rows, total_rows));
-    l.few = !l.rows || n_seqs > 1;
-    l.few_bytes = align_up(iso_attn_kv4_few_ws_bytes(c.head_dim, ncu), 256);
-    l.rows_bytes = many(total_rows) ? iso_attn_kv4_rows_ws_bytes(c.n_kv_heads, c.head_dim, ncu) : 0;
-    return l;
-}
-
 }  // namespace
 
 extern "C" {
@@ -1450,8 +1432,7 @@ int iso_attn_kv4_workspace(iso_ctx *ctx, int n_seqs, int total_rows, size_t *byt
     if (total_rows < 1) return fail(ISO_ERR_SHAPE, "total_rows=%d must be positive", total_rows);
     if ((long long)total_rows * ctx->cfg.n_q_heads >= (1ll << 31))
         return fail(ISO_ERR_SHAPE, "total_rows=%d of %d heads: fewer than 2^31 together", total_rows, ctx->cfg.n_q_heads);
-    const Kv4Launch l = kv4_launch(ctx->cfg, n_seqs, total_rows, total_rows);
-    *bytes = l.few_bytes + l.rows_bytes;
+    *bytes = iso_attn_kv4_ws_bytes(ctx->cfg.dtype, ctx->cfg.n_kv_heads, ctx->cfg.head_dim, iso_num_cu());
     return ISO_OK;
 }
 
@@ -1478,15 +1459,10 @@ int iso_attn_kv4(iso_ctx *ctx, const void *q, int q_stride, const iso_kv4 *cache
     if (ctx->flags & ISO_FLAG_SIMPLE_ATTN) {
         LAUNCH_TRY(ISO_K_ATTN, s, iso_launch_attn_kv4_simple(c.dtype, q, q_stride, *cache, b, out, c.n_q_heads, c.n_kv_heads, c.head_dim, s),
                    "kv4 attention");
-        return ISO_OK;
+    } else {
+        LAUNCH_TRY(ISO_K_ATTN, s, iso_launch_attn_kv4(c.dtype, q, q_stride, *cache, b, std::min(max_rows, total_rows), out, c.n_q_heads, c.n_kv_heads,
+                                                      c.head_dim, ws, s), "kv4 attention");
     }
-    const Kv4Launch l = kv4_launch(c, n_seqs, total_rows, max_rows);
-    if (l.few)
-        LAUNCH_TRY(ISO_K_ATTN, s, iso_launch_attn_kv4_few(c.dtype, q, q_stride, *cache, b, l.rows ? KV4_FEW : 0x7fffffff, out, c.n_q_heads, c.n_kv_heads,
-                                                          c.head_dim, ws, s), "kv4 attention");
-    if (l.rows)
-        LAUNCH_TRY(ISO_K_ATTN, s, iso_launch_attn_kv4_rows(q, q_stride, *cache, b, l.few ? KV4_FEW : 0, out, c.n_q_heads, c.n_kv_heads, c.head_dim,
-                                                           (char *)ws + l.few_bytes, s), "kv4 attention, many rows");
     return ISO_OK;
 }
 
