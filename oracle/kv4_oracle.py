@@ -76,18 +76,24 @@ def attention(q, k, v, table, page, row_start, kv_len, group, n_pages=None):
     n_pages = len(k) if n_pages is None else n_pages
     for i, n_keys in enumerate(kv_len):
         lo, hi = int(row_start[i]), int(row_start[i + 1])
-        for r in range(max(lo, 0), min(hi, rows)):
-            keys = [j for j in range(min(int(n_keys), int(n_keys) - (hi - lo) + (r - lo) + 1, table.shape[1] * page))
-                    if 0 <= table[i, j // page] < n_pages]
-            out[r], spread[r], reach[r] = 0.0, 0.0, 0.0
-            if not keys:
-                continue
-            pg, at = table[i, np.array(keys) // page], np.array(keys) % page
-            for h in range(nq):
-                kk, vv = k[pg, h // group, at], v[pg, h // group, at]
-                s = kk @ q[r, h] / np.sqrt(d)
-                p = np.exp(s - s.max())
-                p /= p.sum()
-                out[r, h], spread[r, h] = p @ vv, p @ np.abs(vv)
-                reach[r, h] = (np.abs(kk) @ np.abs(q[r, h])).max() / np.sqrt(d)
+        r = np.arange(max(lo, 0), min(hi, rows))
+        if not r.size:
+            continue
+        keys = np.arange(min(max(int(n_keys), 0), table.shape[1] * page))
+        pg = table[i, keys // page]
+        there = (pg >= 0) & (pg < n_pages)
+        keys, pg = keys[there], pg[there]
+        seen = keys[None] <= int(n_keys) - (hi - lo) + (r - lo)[:, None]           # [rows, keys]
+        some = seen.any(1)
+        out[r], spread[r], reach[r] = 0.0, 0.0, 0.0
+        if not some.any():
+            continue
+        r, seen = r[some], seen[some]
+        for h in range(nq):
+            kk, vv = k[pg, h // group, keys % page], v[pg, h // group, keys % page]
+            s = np.where(seen, q[r, h] @ kk.T / np.sqrt(d), -np.inf)
+            p = np.exp(s - s.max(1, keepdims=True))
+            p /= p.sum(1, keepdims=True)
+            out[r, h], spread[r, h] = p @ vv, p @ np.abs(vv)
+            reach[r, h] = np.where(seen, np.abs(q[r, h]) @ np.abs(kk).T, 0.0).max(1) / np.sqrt(d)
     return out, spread, reach

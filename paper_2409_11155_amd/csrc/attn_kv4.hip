@@ -49,6 +49,7 @@ struct line_args {
     kv4_view c;
     kv4_batch b;
     int q_stride, nq, nkv, G;            // G: query heads of a key head
+    int most;                            // requests of more (row, head) pairs than this belong to another launch
 };
 
 __device__ __forceinline__ bf16x4_v read_tr(unsigned addr) {
@@ -134,7 +135,7 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
     auto request = [&](int i) {
         const kv4_rows r = kv4_rows_of(scalar(b.row_start), scalar(b.kv_len), b.total_rows, i);
         const int keys = kv4_keys_of(scalar(b.kv_len), b.max_pages, i, shift), base = min(r.base, keys);
-        return Req{r.first, r.n, base, keys, (unsigned)(r.n * G + ROWS - 1) / ROWS, (u64)(unsigned)G * ((unsigned)max(0, base) + 1u + SETUP)};
+        return Req{r.first, r.n, base, keys, r.n * G > a.most ? 0u : (unsigned)(r.n * G + ROWS - 1) / ROWS, (u64)(unsigned)G * ((unsigned)max(0, base) + 1u + SETUP)};
     };
     auto places = [](const Req &q, unsigned k) { return k * q.start + (u64)ROWS * ((u64)k * (k + 1) / 2); };      // of the first k tiles
     auto of_lane = [&](int i) { return i < b.n_seqs ? places(request(i), request(i).tiles) : 0; };
@@ -583,10 +584,10 @@ size_t iso_attn_kv4_ws_bytes(int dtype, int nkv, int d, int ncu) {
     return most;
 }
 
-hipError_t iso_launch_attn_kv4(int dtype, const void *q, int q_stride, const iso_kv4 &cache, const kv4_batch &b, int max_rows, void *out, int nq,
-                               int nkv, int d, void *ws, hipStream_t s) {
-    const line_args a{q, out, nullptr, nullptr, kv4_view_of(cache), b, q_stride, nq, nkv, nq / nkv};
-    const bool two = (long long)max_rows * a.G > 16;
+hipError_t iso_launch_attn_kv4(int dtype, const void *q, int q_stride, const iso_kv4 &cache, const kv4_batch &b, int max_rows, int most, void *out,
+                               int nq, int nkv, int d, void *ws, hipStream_t s) {
+    const line_args a{q, out, nullptr, nullptr, kv4_view_of(cache), b, q_stride, nq, nkv, nq / nkv, most};
+    const bool two = std::min((long long)max_rows * a.G, (long long)most) > 16;
     if (dtype == ISO_F32) return d == 64 ? launch<float, 64, 1>(a, ws, s) : launch<float, 128, 1>(a, ws, s);
     if (d == 64) return two ? launch<bf16_t, 64, 2>(a, ws, s) : launch<bf16_t, 64, 1>(a, ws, s);
     return two ? launch<bf16_t, 128, 2>(a, ws, s) : launch<bf16_t, 128, 1>(a, ws, s);

@@ -875,6 +875,28 @@ int check_kv4(const iso_kv4 *c) {
     return ISO_OK;
 }
 
+// Which kernels a batch needs, and their regions of its workspace (both are there whatever max_rows says).  Long chunks go to the tiles
+// of 128 rows: 8 heads, 2048 rows over 2048 / 8192 / 32768 keys 33 / 93 / 350 us, with 32 rows a tile 35 / 119 / 440; 16 heads, 1024 rows over 6000
+// keys 78 and 98; but 509 over 700 keys 39 and 21, 16 over 8192 47 and 26: they need many row tiles.  Shorter requests of such a batch
+// stay with the other kernel, which costs a second launch.
+struct Kv4Launch {
+    bool line, rows;
+    int most;                      // pairs of (row, query head of a key head) up to which a request belongs to the line
+    size_t line_bytes, rows_bytes;
+};
+Kv4Launch kv4_launch(const iso_cfg &c, int n_seqs, int total_rows, int max_rows) {
+    const int ncu = iso_num_cu();
+    const bool can = c.dtype == ISO_BF16 && c.n_q_heads / c.n_kv_heads <= 64;
+    auto many = [&](int rows) { return can && (long long)rows * c.n_q_heads >= 16384; };
+    Kv4Launch l;
+    l.rows = many(n_seqs == 1 ? total_rows : std::min(max_rows, total_rows));
+    l.line = !l.rows || n_seqs > 1;
+    l.most = !l.rows ? 0x7fffffff : l.line ? 1023 : 0;
+    l.line_bytes = align_up(iso_attn_kv4_ws_bytes(c.dtype, c.n_kv_heads, c.head_dim, ncu), 256);
+    l.rows_bytes = many(total_rows) ? iso_attn_kv4_rows_ws_bytes(c.n_kv_heads, c.head_dim, ncu) : 0;
+    return l;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1432,7 +1454,8 @@ int iso_attn_kv4_workspace(iso_ctx *ctx, int n_seqs, int total_rows, size_t *byt
     if (total_rows < 1) return fail(ISO_ERR_SHAPE, "total_rows=%d must be positive", total_rows);
     if ((long long)total_rows * ctx->cfg.n_q_heads >= (1ll << 31))
         return fail(ISO_ERR_SHAPE, "total_rows=%d of %d heads: fewer than 2^31 together", total_rows, ctx->cfg.n_q_heads);
-    *bytes = iso_attn_kv4_ws_bytes(ctx->cfg.dtype, ctx->cfg.n_kv_heads, ctx->cfg.head_dim, iso_num_cu());
+    const Kv4Launch l = kv4_launch(ctx->cfg, n_seqs, total_rows, total_rows);
+    *bytes = l.line_bytes + l.rows_bytes;
     return ISO_OK;
 }
 
@@ -1459,10 +1482,15 @@ int iso_attn_kv4(iso_ctx *ctx, const void *q, int q_stride, const iso_kv4 *cache
     if (ctx->flags & ISO_FLAG_SIMPLE_ATTN) {
         LAUNCH_TRY(ISO_K_ATTN, s, iso_launch_attn_kv4_simple(c.dtype, q, q_stride, *cache, b, out, c.n_q_heads, c.n_kv_heads, c.head_dim, s),
                    "kv4 attention");
-    } else {
-        LAUNCH_TRY(ISO_K_ATTN, s, iso_launch_attn_kv4(c.dtype, q, q_stride, *cache, b, std::min(max_rows, total_rows), out, c.n_q_heads, c.n_kv_heads,
-                                                      c.head_dim, ws, s), "kv4 attention");
+        return ISO_OK;
     }
+    const Kv4Launch l = kv4_launch(c, n_seqs, total_rows, max_rows);
+    if (l.line)
+        LAUNCH_TRY(ISO_K_ATTN, s, iso_launch_attn_kv4(c.dtype, q, q_stride, *cache, b, std::min(max_rows, total_rows), l.most, out, c.n_q_heads,
+                                                      c.n_kv_heads, c.head_dim, ws, s), "kv4 attention");
+    if (l.rows)
+        LAUNCH_TRY(ISO_K_ATTN, s, iso_launch_attn_kv4_rows(q, q_stride, *cache, b, l.most, out, c.n_q_heads, c.n_kv_heads, c.head_dim,
+                                                           (char *)ws + l.line_bytes, s), "kv4 attention, many rows");
     return ISO_OK;
 }
 

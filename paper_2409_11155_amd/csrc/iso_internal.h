@@ -216,9 +216,13 @@ hipError_t iso_launch_kv4_load(int dtype, const iso_kv4 &cache, const int *slots
 hipError_t iso_launch_attn_kv4_simple(int dtype, const void *q, int q_stride, const iso_kv4 &cache, const kv4_batch &b, void *out, int nq,
                                       int nkv, int d, hipStream_t s);
 size_t iso_attn_kv4_ws_bytes(int dtype, int nkv, int d, int ncu);
-// max_rows: most rows of a request, as far as known
-hipError_t iso_launch_attn_kv4(int dtype, const void *q, int q_stride, const iso_kv4 &cache, const kv4_batch &b, int max_rows, void *out, int nq,
-                               int nkv, int d, void *ws, hipStream_t s);
+// requests of at most `most` (row, query head of a key head) pairs; max_rows: most rows of a request, as far as known
+hipError_t iso_launch_attn_kv4(int dtype, const void *q, int q_stride, const iso_kv4 &cache, const kv4_batch &b, int max_rows, int most, void *out,
+                               int nq, int nkv, int d, void *ws, hipStream_t s);
+// bf16, requests of more than `most` pairs, at most 64 query heads of a key head
+size_t iso_attn_kv4_rows_ws_bytes(int nkv, int d, int ncu);
+hipError_t iso_launch_attn_kv4_rows(const void *q, int q_stride, const iso_kv4 &cache, const kv4_batch &b, int most, void *out, int nq, int nkv,
+                                    int d, void *ws, hipStream_t s);
 
 // ---- small device helpers ----------------------------------------------------------------------
 __device__ __forceinline__ float iso_to_f32(float v) { return v; }

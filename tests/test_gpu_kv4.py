@@ -187,7 +187,8 @@ def fill(n_pages, nkv, page, d, seed, table=None, kv=None):
     rng = np.random.default_rng(seed)
     codes, scales = [], []
     for _ in range(2):
-        c, s = ko.encode(rng.standard_normal((n_pages, nkv, page, d)))
+        pick = rng.integers(0, min(n_pages, 40), n_pages)        # pages drawn from a few that are encoded
+        c, s = (a[pick] for a in ko.encode(rng.standard_normal((min(n_pages, 40), nkv, page, d))))
         used = np.zeros((n_pages, page), bool)
         for i, n in enumerate(kv):
             j = np.arange(min(max(int(n), 0), table.shape[1] * page))
@@ -312,3 +313,98 @@ def test_a_token_that_holds_nan_reaches_only_the_rows_that_see_it(dt, heads, fla
     assert not np.isnan(got[:sees]).any()
     if nkv > 1:
         assert not np.isnan(got[:, : nq - nq // nkv, :32]).any()
+
+
+# ------------------------------------------------------------------------------------------------ long chunks: tiles of 128 rows
+
+# rows x query heads from 16384 on: head layouts with many heads reach it with few rows
+MANY = [(64, 1, 64), (64, 64, 64), (64, 2, 128), (66, 22, 128), (104, 8, 64)]
+LONG = {
+    "fresh": ([256], [256], 64),
+    "odd": ([1301], [257], 16),
+    "two": ([290, 1000], [290, 259], 256),
+    "mixed": ([700, 40, 1, 901, 77, 0], [300, 1, 1, 2, 0, 3], 32),
+    "short_of_tokens": ([100], [256], 64),                       # the first 156 rows see nothing
+}
+
+
+@pytest.mark.parametrize("heads", MANY)
+@pytest.mark.parametrize("name", LONG)
+def test_long_chunks(heads, name):
+    nq, nkv, d = heads
+    kv, fresh, page = LONG[name]
+    table, row_start, n_pages = batch(kv, fresh, page, seed=len(name))
+    codes, scales = fill(n_pages, nkv, page, d, 7, table, kv)
+    q = iso_inputs.randn((int(row_start[-1]), nq, d), seed=9, dtype="bf16")
+    with make_ctx(nq, nkv, d, "bf16") as ctx:
+        cache = device_cache(codes, scales, page)
+        ws = iso.DeviceArray((ctx.attn_kv4_workspace(len(kv), q.shape[0]),), "u8", fill_byte=0)
+        out = [attend(ctx, q, cache, table, row_start, kv, "bf16", nq, d, ws=ws).numpy() for _ in range(3)]
+    np.testing.assert_array_equal(out[0], out[1])                # the workspace is left ready, the order of arrivals does not show
+    np.testing.assert_array_equal(out[0], out[2])
+    ref = check(f64(out[0], "bf16"), f64(q, "bf16"), ko.decode(codes[0], scales[0]), ko.decode(codes[1], scales[1]), table, page, row_start, kv,
+                nq // nkv, "bf16", n_pages)
+    assert (f64(out[0], "bf16")[(ref == 0).all((1, 2))] == 0).all()
+
+
+@pytest.mark.parametrize("heads", [(64, 1, 64), (64, 2, 128)])
+@pytest.mark.parametrize("kv,fresh,bad", [(900, 260, 700), (900, 260, 30), (256, 256, 0)])
+def test_long_chunks_with_a_nan_and_missing_pages(heads, kv, fresh, bad):
+    nq, nkv, d = heads
+    page = 16
+    table, row_start, n_pages = batch([kv], [fresh], page, seed=5)
+    row_start = row_start + 1
+    gone = [2, 9] if kv > 300 else [5]
+    table[0, gone] = [-1, n_pages][: len(gone)]
+    codes, scales = fill(n_pages, nkv, page, d, 6, table, [kv])
+    clean = scales[1].copy()
+    scales[1][table[0, bad // page], :, bad % page, 1] = 255
+    q = iso_inputs.randn((fresh + 3, nq, d), seed=4, dtype="bf16")
+    with make_ctx(nq, nkv, d, "bf16") as ctx:
+        out = attend(ctx, q, device_cache(codes, scales, page), table, row_start, [kv], "bf16", nq, d)
+    got = f64(out, "bf16")
+    sees = 1 + max(0, bad - (kv - fresh))
+    assert np.isnan(got[sees:-2, :, 32:64]).all() and not np.isnan(got[1:sees]).any()
+    k, v = ko.decode(codes[0], scales[0]), ko.decode(codes[1], clean)
+    without = ko.attention(f64(q, "bf16"), k, v, table, page, row_start, [kv], nq // nkv, n_pages)[0]
+    inside = np.where(np.isnan(got), without, got)
+    check(inside, f64(q, "bf16"), k, v, table, page, row_start, [kv], nq // nkv, "bf16", n_pages)
+    assert (out.numpy().view(np.uint8).reshape(fresh + 3, -1)[[0, -2, -1]] == 0xFF).all()
+    assert not np.isnan(got[1:-2, :, :32]).any()
+
+
+@pytest.mark.parametrize("dt,heads", [("bf16", (8, 1, 128)), ("bf16", (3, 3, 128)), ("bf16", (16, 4, 64)), ("f32", (4, 2, 64))])
+@pytest.mark.parametrize("kv,fresh", [([40000], [1]), ([9000, 3, 20011], [1, 1, 6]), ([900] * 33, [1] * 33)])
+def test_many_pieces_and_one_workspace_for_all(dt, heads, kv, fresh):
+    """Keys dealt to hundreds of workgroups and folded in two rounds; calls of other shapes on the same workspace in between."""
+    nq, nkv, d = heads
+    page = 64
+    table, row_start, n_pages = batch(kv, fresh, page, seed=2)
+    codes, scales = fill(n_pages, nkv, page, d, 3, table, kv)
+    q = iso_inputs.randn((int(row_start[-1]), nq, d), seed=9, dtype=dt)
+    other = batch([300, 77], [40, 1], page, seed=4)
+    with make_ctx(nq, nkv, d, dt) as ctx:
+        cache = device_cache(codes, scales, page)
+        ws = iso.DeviceArray((max(ctx.attn_kv4_workspace(len(kv), q.shape[0]), ctx.attn_kv4_workspace(2, 41)),), "u8", fill_byte=0)
+        out = []
+        for _ in range(3):
+            out.append(attend(ctx, q, cache, table, row_start, kv, dt, nq, d, ws=ws).numpy())
+            attend(ctx, iso_inputs.randn((41, nq, d), seed=1, dtype=dt), cache, other[0] % n_pages, other[1], [300, 77], dt, nq, d, ws=ws)
+    np.testing.assert_array_equal(out[0], out[1])
+    np.testing.assert_array_equal(out[0], out[2])
+    check(f64(out[0], dt), f64(q, dt), ko.decode(codes[0], scales[0]), ko.decode(codes[1], scales[1]), table, page, row_start, kv, nq // nkv, dt, n_pages)
+
+
+@pytest.mark.parametrize("n_seqs", [64, 65, 200, 4096])
+def test_many_requests(n_seqs):
+    """More requests than a wave has lanes; every third has no row, lengths from one."""
+    nq, nkv, d, page, dt = 4, 2, 64, 16, "bf16"
+    rng = np.random.default_rng(n_seqs)
+    kv = rng.integers(1, 60, n_seqs)
+    fresh = np.where(np.arange(n_seqs) % 3 == 1, 0, np.minimum(kv, rng.integers(1, 4, n_seqs)))
+    table, row_start, n_pages = batch(list(kv), list(fresh), page, seed=1)
+    codes, scales = fill(n_pages, nkv, page, d, 3, table, kv)
+    q = iso_inputs.randn((int(row_start[-1]), nq, d), seed=9, dtype=dt)
+    with make_ctx(nq, nkv, d, dt) as ctx:
+        got = f64(attend(ctx, q, device_cache(codes, scales, page), table, row_start, list(kv), dt, nq, d), dt)
+    check(got, f64(q, dt), ko.decode(codes[0], scales[0]), ko.decode(codes[1], scales[1]), table, page, row_start, list(kv), nq // nkv, dt, n_pages)
