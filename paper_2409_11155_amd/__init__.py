@@ -267,6 +267,9 @@ class DeviceArray:
     def data_ptr(self) -> int:
         return self.ptr
 
+    def is_contiguous(self) -> bool:
+        return True
+
     def free(self) -> None:
         if getattr(self, "ptr", None):
             self._lib.iso_dev_free(self.ptr)
@@ -328,14 +331,14 @@ class Stream:
 
 
 def _ptr(t) -> Optional[int]:
-    if type(t) is DeviceArray:
-        return t.ptr
-    if t is None or isinstance(t, int):
-        return t
-    contiguous = getattr(t, "is_contiguous", None)
-    if contiguous is not None and not contiguous():
-        raise ValueError("libiso takes contiguous buffers")
-    return t.data_ptr()
+    if t is None:
+        return None
+    try:                                                # a step makes dozens of these: device buffers without a type test
+        if t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        return t if isinstance(t, int) else t.data_ptr()
+    raise ValueError("libiso takes contiguous buffers")
 
 
 def copy_d2h_async(dst: "PinnedArray", src: "DeviceArray", nbytes: int, stream) -> None:
@@ -348,9 +351,10 @@ def _stream_handle(s) -> Optional[int]:
         return None
     if isinstance(s, Stream):
         return s.handle
-    if hasattr(s, "cuda_stream"):
+    try:
         return s.cuda_stream or None
-    return int(s) or None
+    except AttributeError:
+        return int(s) or None
 
 
 def pack_weights(w: Dict[str, object]) -> IsoWeights:
@@ -376,6 +380,7 @@ class Kv4Cache:
         self.page, self.n_pages, self.nkv, self.head_dim = page, shapes[0][0], shapes[0][1], 2 * shapes[0][3]
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale      # kept alive
         self.handle = IsoKv4(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), self.n_pages, page)
+        self.ref = ctypes.byref(self.handle)
 
 
 class Context:
@@ -522,9 +527,10 @@ class Context:
         return Kv4Cache(page, k, v, ks, vs)
 
     def _kv4(self, cache: Kv4Cache):
-        if (cache.nkv, cache.head_dim) != (self.cfg.n_kv_heads, self.cfg.head_dim):
-            raise ValueError(f"a cache of {cache.nkv} heads of {cache.head_dim}, the context has {self.cfg.n_kv_heads} of {self.cfg.head_dim}")
-        return ctypes.byref(cache.handle)
+        cfg = self.cfg
+        if cache.nkv != cfg.n_kv_heads or cache.head_dim != cfg.head_dim:
+            raise ValueError(f"a cache of {cache.nkv} heads of {cache.head_dim}, the context has {cfg.n_kv_heads} of {cfg.head_dim}")
+        return cache.ref
 
     def block_tables(self, cached, fresh, n_seqs: int, page: int, free_pages, n_free: int, free_head, block_table, max_pages: int, row_start,
                      kv_len, positions, slots, max_rows: int, free_next, stream=None) -> None:

@@ -864,6 +864,13 @@ int check_device(const iso_ctx *ctx) {
     return ISO_OK;
 }
 
+// Rows of a write or a read: (row, head) pairs are counted in 31 bits.
+int check_rows(const iso_cfg &c, int T) {
+    if (T < 1) return fail(ISO_ERR_SHAPE, "T=%d must be positive", T);
+    if ((long long)T * (c.n_q_heads + 2 * c.n_kv_heads) >= (1ll << 31)) return fail(ISO_ERR_SHAPE, "T=%d rows of %d heads: fewer than 2^31 together", T, c.n_q_heads + 2 * c.n_kv_heads);
+    return ISO_OK;
+}
+
 int check_kv4(const iso_kv4 *c) {
     if (!c) return fail(ISO_ERR_NULL, "cache is NULL");
     if (!c->k || !c->v || !c->k_scale || !c->v_scale) return fail(ISO_ERR_NULL, "the cache's k, v, k_scale and v_scale must be non-NULL");
@@ -1411,7 +1418,7 @@ int iso_rope_kv4_write(iso_ctx *ctx, void *qkv, void *q_out, const iso_kv4 *cach
     if (!ctx) return fail(ISO_ERR_NULL, "ctx is NULL");
     if (!qkv || !positions || !slots) return fail(ISO_ERR_NULL, "qkv, positions and slots must be non-NULL");
     ISO_TRY(check_kv4(cache));
-    if (T < 1) return fail(ISO_ERR_SHAPE, "T=%d must be positive", T);
+    ISO_TRY(check_rows(ctx->cfg, T));
     if (!aligned(qkv, 16) || !aligned(q_out, 16) || !aligned(positions, 4) || !aligned(slots, 4))
         return fail(ISO_ERR_SHAPE, "qkv and q_out must be 16-byte aligned, positions and slots 4-byte");
     ISO_TRY(check_device(ctx));
@@ -1426,7 +1433,7 @@ int iso_kv4_store(iso_ctx *ctx, const void *k, const void *v, const iso_kv4 *cac
     if (!ctx) return fail(ISO_ERR_NULL, "ctx is NULL");
     if (!k || !v || !slots) return fail(ISO_ERR_NULL, "k, v and slots must be non-NULL");
     ISO_TRY(check_kv4(cache));
-    if (T < 1) return fail(ISO_ERR_SHAPE, "T=%d must be positive", T);
+    ISO_TRY(check_rows(ctx->cfg, T));
     if (!aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 4)) return fail(ISO_ERR_SHAPE, "k and v must be 16-byte aligned, slots 4-byte");
     ISO_TRY(check_device(ctx));
     const iso_cfg &c = ctx->cfg;
@@ -1439,7 +1446,7 @@ int iso_kv4_load(iso_ctx *ctx, const iso_kv4 *cache, const int *slots, void *k, 
     if (!ctx) return fail(ISO_ERR_NULL, "ctx is NULL");
     if (!k || !v || !slots) return fail(ISO_ERR_NULL, "k, v and slots must be non-NULL");
     ISO_TRY(check_kv4(cache));
-    if (T < 1) return fail(ISO_ERR_SHAPE, "T=%d must be positive", T);
+    ISO_TRY(check_rows(ctx->cfg, T));
     if (!aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 4)) return fail(ISO_ERR_SHAPE, "k and v must be 16-byte aligned, slots 4-byte");
     ISO_TRY(check_device(ctx));
     const iso_cfg &c = ctx->cfg;

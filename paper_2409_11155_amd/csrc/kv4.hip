@@ -130,11 +130,11 @@ __device__ __forceinline__ void store8(bf16_t *p, const float (&x)[8]) {
 // Rounds to fp32 so that no comparison with a number of fewer bits comes out otherwise than for x itself: toward zero, and the
 // last bit set if something was cut off.  (Nearest would take a value just beside the border of two codes onto it.)
 __device__ __forceinline__ float round_to_odd(double x) {
-    if (isfinite(x)) x = fmin(fmax(x, -(double)3.4e38f), (double)3.4e38f);      // beyond it every code saturates alike
     const float f = (float)x;
-    const double back = (double)f;
-    if (back == x || !isfinite(x)) return f;
-    return __uint_as_float((__float_as_uint(f) - (fabs(back) > fabs(x) ? 1u : 0u)) | 1u);
+    if (!(fabsf(f) < INFINITY)) return isfinite(x) ? copysignf(3.4e38f, f) : f;      // beyond it every code saturates alike
+    const double cut = x - (double)f;                  // exact
+    const unsigned away = (unsigned)(__double2hiint(cut) ^ __double2hiint(x)) >> 31;  // rounded away from zero
+    return cut == 0.0 ? f : __uint_as_float((__float_as_uint(f) - away) | 1u);
 }
 
 // Codes and scale of the block that four neighbouring lanes hold: e = least integer with max|x| <= 7 * 2^e.  (7 and not 6: what lies
@@ -166,13 +166,22 @@ template <int D> __device__ __forceinline__ size_t token_at(const kv4_view &c, i
     return (((size_t)(slot >> c.page_shift) * nkv + g) << c.page_shift) + (slot & (c.page - 1));
 }
 
+// Both halves of a head that its lanes hold, to token `tok`: four bytes of codes a lane and half; the scales of all blocks go to the
+// first lane, which stores them at once.
 template <int D>
-__device__ __forceinline__ void put_half(unsigned char *codes, unsigned char *scales, size_t tok, const float (&x)[8], int l, int hi) {
-    unsigned s;
-    const unsigned w = encode8(x, &s);
-    const int e0 = hi * (D / 2) + 8 * l;               // first element
-    *reinterpret_cast<unsigned *>(codes + tok * (D / 2) + e0 / 2) = w;
-    if ((l & 3) == 0) scales[tok * (D / KV4_BLOCK) + e0 / KV4_BLOCK] = (unsigned char)s;
+__device__ __forceinline__ void put(unsigned char *codes, unsigned char *scales, size_t tok, const float (&lo)[8], const float (&hi)[8], int l) {
+    unsigned s_lo, s_hi;
+    unsigned *const w = reinterpret_cast<unsigned *>(codes + tok * (D / 2));
+    const unsigned c_lo = encode8(lo, &s_lo), c_hi = encode8(hi, &s_hi);
+    w[l] = c_lo;
+    w[D / 16 + l] = c_hi;
+    if constexpr (D == 128) {                          // lanes 0 and 4: blocks 0 | 2 and 1 | 3
+        const unsigned mine = s_lo | s_hi << 16;
+        const unsigned next = (unsigned)__builtin_amdgcn_mov_dpp((int)mine, 0x104, 0xF, 0xF, true);      // from four lanes up
+        if (l == 0) reinterpret_cast<unsigned *>(scales)[tok] = mine | next << 8;
+    } else {
+        if (l == 0) reinterpret_cast<unsigned short *>(scales)[tok] = (unsigned short)(s_lo | s_hi << 8);
+    }
 }
 
 // ROPE: rows of the QKV projection, heads [q | k | v]; q is rotated into q_out (or in place), k rotated, both written at `slots`.
@@ -185,24 +194,23 @@ __global__ __launch_bounds__(256) void kv4_write_kernel(T *qkv, T *q_out, const 
                                                         const float *__restrict__ cos_t, const float *__restrict__ sin_t, int max_pos,
                                                         int n_rows, int nq, int nkv) {
     constexpr int LPH = D / 16;                        // lanes per head
-    const int heads = ROPE ? nq + 2 * nkv : 2 * nkv;
-    const long long u = (long long)blockIdx.x * 256 + threadIdx.x;
-    const long long th = u / LPH;
-    const int l = (int)(u % LPH);
-    if (th >= (long long)n_rows * heads) return;       // a head's lanes leave together
-    const int t = (int)(th / heads), h = (int)(th % heads);
+    const unsigned heads = ROPE ? nq + 2 * nkv : 2 * nkv;
+    const unsigned th = blockIdx.x * (256u / LPH) + threadIdx.x / LPH;         // (row, head); fewer than 2^31 of them
+    const int l = threadIdx.x % LPH;
+    if (th >= (unsigned)n_rows * heads) return;        // a head's lanes leave together
+    const int t = (int)(th / heads), h = (int)(th - (unsigned)t * heads);
     const int nqk = ROPE ? nq + nkv : nkv;             // heads in front of v
     const bool is_q = ROPE && h < nq, is_v = h >= nqk;
     const int g = is_q ? 0 : is_v ? h - nqk : ROPE ? h - nq : h;
-    const T *src = ROPE ? qkv + ((size_t)t * heads + h) * D : (is_v ? v_rows : k_rows) + ((size_t)t * nkv + g) * D;
+    const T *src = ROPE ? qkv + (size_t)th * D : (is_v ? v_rows : k_rows) + ((size_t)t * nkv + g) * D;
+    float lo[8], hi[8];
+    load8<T>(src + 8 * l, lo);                         // on their way before it is known where they go
+    load8<T>(src + D / 2 + 8 * l, hi);
     const int slot = slots[t];
     const bool kept = slot >= 0 && (slot >> c.page_shift) < c.n_pages;
     const int pos = ROPE ? positions[t] : 0;
     if (pos < 0 || pos >= max_pos) return;             // no row
     if (!is_q && !kept) return;
-    float lo[8], hi[8];
-    load8<T>(src + 8 * l, lo);
-    load8<T>(src + D / 2 + 8 * l, hi);
     if (ROPE && !is_v) {
         float cs[8], sn[8];
         load8<float>(cos_t + (size_t)pos * (D / 2) + 8 * l, cs);
@@ -227,8 +235,7 @@ __global__ __launch_bounds__(256) void kv4_write_kernel(T *qkv, T *q_out, const 
         }
     }
     const size_t tok = token_at<D>(c, nkv, slot, g);
-    put_half<D>(is_v ? c.v : c.k, is_v ? c.vs : c.ks, tok, lo, l, 0);
-    put_half<D>(is_v ? c.v : c.k, is_v ? c.vs : c.ks, tok, hi, l, 1);
+    put<D>(is_v ? c.v : c.k, is_v ? c.vs : c.ks, tok, lo, hi, l);
 }
 
 // The values that the slots hold, as rows: eight elements a lane.
@@ -236,11 +243,10 @@ template <typename T, int D>
 __global__ __launch_bounds__(256) void kv4_load_kernel(kv4_view c, const int *__restrict__ slots, T *__restrict__ k_rows,
                                                        T *__restrict__ v_rows, int n_rows, int nkv) {
     constexpr int LPH = D / 8;
-    const long long u = (long long)blockIdx.x * 256 + threadIdx.x;
-    const long long th = u / LPH;
-    const int l = (int)(u % LPH);
-    if (th >= (long long)n_rows * 2 * nkv) return;
-    const int t = (int)(th / (2 * nkv)), h = (int)(th % (2 * nkv));
+    const unsigned th = blockIdx.x * (256u / LPH) + threadIdx.x / LPH;         // (row, head); fewer than 2^31 of them
+    const int l = threadIdx.x % LPH;
+    if (th >= (unsigned)n_rows * 2u * nkv) return;
+    const int t = (int)(th / (2u * nkv)), h = (int)(th - (unsigned)t * (2u * nkv));
     const bool is_v = h >= nkv;
     const int g = is_v ? h - nkv : h;
     const int slot = slots[t];
