@@ -33,6 +33,7 @@ typedef unsigned u32x2_v __attribute__((ext_vector_type(2)));
 constexpr int WAVES = 4, THREADS = 64 * WAVES, TILE = 32, UNIT = WAVES * TILE;
 constexpr int GROUP = 16;                // pieces that are folded at once; a tile has up to GROUP * GROUP of them
 constexpr int SETUP = 512;            // what a tile's start and end cost, in keys
+constexpr int ROUND = 256;            // keys that cost what a second round of folding does: 18 rows, 7300 keys each, 22.4 us with two, 17.1 with one
 constexpr int MIN_SHARE = 256;         // keys of a share, at least
 constexpr int COHERENT = 1 | 16;         // buffer cache policy sc0 | sc1: system scope, bypasses the XCD-local L2
 constexpr int SPLITS = GROUP * GROUP - 2;      // shares that the longest tile is cut into, at most (a share may begin and end inside it)
@@ -151,8 +152,12 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
     const u64 all = lane_of(incl, 63);
     longest = lane_of(wave_scan(longest, [](u64 x, u64 y) { return max(x, y); }), 63);
     // any share does that covers the line; never less than MIN_SHARE keys, nor so little that a tile has more pieces than can be folded
-    const u64 per = uniform(max(max((u64)((double)all * (1.000001 * __builtin_amdgcn_rcp((double)gridDim.x))) + 1, (u64)((double)longest * (1.0 / SPLITS)) + 1),
-                                (u64)G * MIN_SHARE));
+    u64 per = max(max((u64)((double)all * (1.000001 * __builtin_amdgcn_rcp((double)gridDim.x))) + 1, (u64)((double)longest * (1.0 / SPLITS)) + 1),
+                  (u64)G * MIN_SHARE);
+    // one round of folding instead of two where that lengthens a share by less than ROUND keys
+    const u64 one_round = (u64)((double)longest * (1.0 / (GROUP - 1))) + 1;
+    if (one_round > per && one_round - per < (u64)G * ROUND) per = one_round;
+    per = uniform(per);
     u64 at = (u64)blockIdx.x * per;
     const u64 end = min(all, at + per);
     if (at >= end) return;
@@ -319,7 +324,8 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
                 };
                 read_v(0, 0);
                 __builtin_amdgcn_sched_barrier(0);
-                bf16x8_t pb[RT][NP];
+                float mx[RT];
+                bool moves = false;
 #pragma unroll
                 for (int x = 0; x < N; ++x) {
                     if (masked) {
@@ -330,23 +336,30 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
                             for (int e = 0; e < 4; ++e) s[x][h][e] = e < vis ? s[x][h][e] : -INFINITY;
                         }
                     }
-                    float mx = -INFINITY;
+                    mx[x] = -INFINITY;
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[x][h][e]);
-                    mx *= sc;
-                    // the running maximum moves rarely deep in a cache; the four lanes of a row agree on it
-                    if (__builtin_amdgcn_ballot_w64(mx > m_run[x]) != 0) {
-                        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-                        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-                        const float m_new = fmaxf(m_run[x], mx);
-                        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[x] - m_new);
-                        m_run[x] = m_new;
+                        for (int e = 0; e < 4; ++e) mx[x] = fmaxf(mx[x], s[x][h][e]);
+                    mx[x] *= sc;
+                    moves = moves || mx[x] > m_run[x];
+                }
+                // the running maximum moves rarely deep in a cache; the four lanes of a row agree on it
+                if (__builtin_amdgcn_ballot_w64(moves) != 0) {
+#pragma unroll
+                    for (int x = 0; x < N; ++x) {
+                        float top = fmaxf(mx[x], __shfl_xor(mx[x], 16, 64));
+                        top = fmaxf(m_run[x], fmaxf(top, __shfl_xor(top, 32, 64)));
+                        const float alpha = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[x] - top);
+                        m_run[x] = top;
                         l_run[x] *= alpha;
 #pragma unroll
                         for (int dt = 0; dt < D / 16; ++dt) o[x][dt] *= alpha;
                     }
+                }
+                bf16x8_t pb[RT][NP];
+#pragma unroll
+                for (int x = 0; x < N; ++x) {
                     const float neg_m = m_run[x] == -INFINITY ? 0.f : -m_run[x];
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
