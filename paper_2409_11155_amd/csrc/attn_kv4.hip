@@ -80,10 +80,10 @@ __device__ __forceinline__ bf16x8_t unpack8(unsigned w, float scale) {
 // Wave-uniform values are made scalar explicitly, and what is read at a uniform place is read by the scalar unit: vector loads come
 // back in order, so a page number among them would have to wait for the codes requested before it.
 typedef const __attribute__((address_space(4))) int *scalar_ints;
-// Buffer over the 4 GB from p + (at & ~0xffffffff) on: with the low half of `at` as the scalar offset, a lane's address is p + at + its own
-// offset without an addition in a vector register.
+// Buffer from p + at on: a lane's address needs no addition in a vector register.  (`at` is not taken as the scalar offset: that one counts
+// in the comparison with the buffer's size, which cannot be more than 4 GB.)
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t beyond(unsigned char *p, uint64_t at) {
-    return __builtin_amdgcn_make_buffer_rsrc((void *)(p + (at & 0xffffffff00000000ull)), 0, -1, 0x00020000);
+    return __builtin_amdgcn_make_buffer_rsrc((void *)(p + at), 0, -1, 0x00020000);
 }
 __device__ __forceinline__ scalar_ints scalar(const int *p) { return (scalar_ints)(uintptr_t)p; }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -260,18 +260,18 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
                     const u64 at_c = tok * (D / 2), at_s = tok * (D / KV4_BLOCK);
                     const auto rk = beyond(a.c.k, at_c), rv = beyond(a.c.v, at_c), rks = beyond(a.c.ks, at_s), rvs = beyond(a.c.vs, at_s);
                     if constexpr (D == 128) {
-                        const u32x4_t x = __builtin_amdgcn_raw_buffer_load_b128(rk, code_at, (unsigned)at_c, 0);
-                        const u32x4_t y = __builtin_amdgcn_raw_buffer_load_b128(rv, code_at, (unsigned)at_c, 0);
+                        const u32x4_t x = __builtin_amdgcn_raw_buffer_load_b128(rk, code_at, 0, 0);
+                        const u32x4_t y = __builtin_amdgcn_raw_buffer_load_b128(rv, code_at, 0, 0);
 #pragma unroll
                         for (int w = 0; w < WPL; ++w) c.k[h][w] = x[w], c.v[h][w] = y[w];
                     } else {
-                        const u32x2_v x = __builtin_amdgcn_raw_buffer_load_b64(rk, code_at, (unsigned)at_c, 0);
-                        const u32x2_v y = __builtin_amdgcn_raw_buffer_load_b64(rv, code_at, (unsigned)at_c, 0);
+                        const u32x2_v x = __builtin_amdgcn_raw_buffer_load_b64(rk, code_at, 0, 0);
+                        const u32x2_v y = __builtin_amdgcn_raw_buffer_load_b64(rv, code_at, 0, 0);
 #pragma unroll
                         for (int w = 0; w < WPL; ++w) c.k[h][w] = x[w], c.v[h][w] = y[w];
                     }
-                    c.ks[h] = __builtin_amdgcn_raw_buffer_load_b8(rks, scale_at, (unsigned)at_s, 0);
-                    c.vs[h] = __builtin_amdgcn_raw_buffer_load_b8(rvs, scale_at, (unsigned)at_s, 0);
+                    c.ks[h] = __builtin_amdgcn_raw_buffer_load_b8(rks, scale_at, 0, 0);
+                    c.vs[h] = __builtin_amdgcn_raw_buffer_load_b8(rvs, scale_at, 0, 0);
                 }
             };
             auto multiply = [&](int k0, Codes &c, auto second_c) {

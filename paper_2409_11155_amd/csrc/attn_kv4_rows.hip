@@ -62,7 +62,7 @@ __device__ __forceinline__ bf16x8_t unpack8(unsigned w, float scale) {
     return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t beyond(unsigned char *p, u64 at) {
-    return __builtin_amdgcn_make_buffer_rsrc((void *)(p + (at & 0xffffffff00000000ull)), 0, -1, 0x00020000);
+    return __builtin_amdgcn_make_buffer_rsrc((void *)(p + at), 0, -1, 0x00020000);
 }
 
 template <int D> __global__ __launch_bounds__(THREADS, 2) void attn_kv4_rows_kernel(rows_args a) {
@@ -206,18 +206,18 @@ template <int D> __global__ __launch_bounds__(THREADS, 2) void attn_kv4_rows_ker
                 const u64 at_c = tok * (D / 2), at_s = tok * (D / KV4_BLOCK);
                 const auto rk = beyond(a.c.k, at_c), rv = beyond(a.c.v, at_c), rks = beyond(a.c.ks, at_s), rvs = beyond(a.c.vs, at_s);
                 if constexpr (D == 128) {
-                    const u32x4_t x = __builtin_amdgcn_raw_buffer_load_b128(rk, code_at, (unsigned)at_c, 0);
-                    const u32x4_t y = __builtin_amdgcn_raw_buffer_load_b128(rv, code_at, (unsigned)at_c, 0);
+                    const u32x4_t x = __builtin_amdgcn_raw_buffer_load_b128(rk, code_at, 0, 0);
+                    const u32x4_t y = __builtin_amdgcn_raw_buffer_load_b128(rv, code_at, 0, 0);
 #pragma unroll
                     for (int w = 0; w < WPL; ++w) c.k[w] = x[w], c.v[w] = y[w];
                 } else {
-                    const u32x2_v x = __builtin_amdgcn_raw_buffer_load_b64(rk, code_at, (unsigned)at_c, 0);
-                    const u32x2_v y = __builtin_amdgcn_raw_buffer_load_b64(rv, code_at, (unsigned)at_c, 0);
+                    const u32x2_v x = __builtin_amdgcn_raw_buffer_load_b64(rk, code_at, 0, 0);
+                    const u32x2_v y = __builtin_amdgcn_raw_buffer_load_b64(rv, code_at, 0, 0);
 #pragma unroll
                     for (int w = 0; w < WPL; ++w) c.k[w] = x[w], c.v[w] = y[w];
                 }
-                c.ks = __builtin_amdgcn_raw_buffer_load_b8(rks, scale_at, (unsigned)at_s, 0);
-                c.vs = __builtin_amdgcn_raw_buffer_load_b8(rvs, scale_at, (unsigned)at_s, 0);
+                c.ks = __builtin_amdgcn_raw_buffer_load_b8(rks, scale_at, 0, 0);
+                c.vs = __builtin_amdgcn_raw_buffer_load_b8(rvs, scale_at, 0, 0);
             };
             auto masked = [&](int k0) { return gaps || k0 + BN > lim_lo; };
             // In a masked tile some row does not see some key: V must hold no NaN there (0 x NaN is NaN); where it does is noted, and

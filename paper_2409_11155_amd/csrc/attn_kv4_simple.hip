@@ -81,7 +81,7 @@ __global__ __launch_bounds__(256) void attn_kv4_simple_kernel(const T *__restric
 hipError_t iso_launch_attn_kv4_simple(int dtype, const void *q, int q_stride, const iso_kv4 &cache, const kv4_batch &b, void *out, int nq,
                                       int nkv, int d, hipStream_t s) {
     const kv4_view c = kv4_view_of(cache);
-    const dim3 grid((b.total_rows + 3) / 4, nq), block(256);
+    const dim3 grid((b.total_rows - 1) / 4 + 1, nq), block(256);
 #define ISO_KV4_SIMPLE(TT, DD) \
     hipLaunchKernelGGL((attn_kv4_simple_kernel<TT, DD>), grid, block, 0, s, (const TT *)q, q_stride, c, b, (TT *)out, nq, nkv)
     if (dtype == ISO_F32 && d == 64) ISO_KV4_SIMPLE(float, 64);

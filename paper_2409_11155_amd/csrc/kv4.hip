@@ -78,22 +78,23 @@ __global__ __launch_bounds__(BT_THREADS) void block_tables_kernel(bt_args a) {
         const long long at = (long long)head + k;
         return at >= 0 && at < a.n_free ? a.free_pages[at] : -1;
     };
-    const int stride = gridDim.x * BT_THREADS;
-    for (int k = blockIdx.x * BT_THREADS + tid; k < p_all; k += stride) {
-        const int i = bt_find(base, a.n_seqs, k);
-        const int col = bt_pages(a.cached[i], a.page_shift, a.max_pages) + k - base[i];
-        if (col < a.max_pages) a.table[(size_t)i * a.max_pages + col] = free_page(k);
+    const unsigned first = blockIdx.x * BT_THREADS + tid, stride = gridDim.x * BT_THREADS;
+    for (unsigned k = first; k < (unsigned)max(0, p_all); k += stride) {
+        const int i = bt_find(base, a.n_seqs, (int)k);
+        const int col = bt_pages(a.cached[i], a.page_shift, a.max_pages) + (int)k - base[i];
+        if ((unsigned)col < (unsigned)a.max_pages) a.table[(size_t)i * a.max_pages + col] = free_page((int)k);
     }
-    for (int r = blockIdx.x * BT_THREADS + tid; r < a.max_rows; r += stride) {
+    for (unsigned x = first; x < (unsigned)a.max_rows; x += stride) {
+        const int r = (int)x;
         int pos = -1, slot = -1;
         if (r < r_all) {
             const int i = bt_find(start, a.n_seqs, r);
             const int c = max(0, a.cached[i]);
             pos = c + r - start[i];
             const int col = pos >> a.page_shift, have = bt_pages(c, a.page_shift, a.max_pages);
-            if (col < a.max_pages) {
+            if ((unsigned)col < (unsigned)a.max_pages) {       // (unsigned: lengths that add up to 2^31 or more stay in bounds too)
                 const int pg = col < have ? a.table[(size_t)i * a.max_pages + col] : free_page(base[i] + col - have);
-                if (pg >= 0) slot = (pg << a.page_shift) + (pos & ((1 << a.page_shift) - 1));
+                if ((unsigned)pg < 0x80000000u >> a.page_shift) slot = (pg << a.page_shift) + (pos & ((1 << a.page_shift) - 1));
             }
         }
         a.positions[r] = pos;
@@ -289,7 +290,7 @@ hipError_t iso_launch_block_tables(const int *cached, const int *fresh, int n_se
                                    int *slots, int max_rows, int *free_next, hipStream_t s) {
     const bt_args a{cached, fresh, free_pages, free_head_or_null, table, row_start, kv_len, positions, slots, free_next,
                     n_seqs, __builtin_ctz((unsigned)page), n_free, max_pages, max_rows};
-    const int wgs = min(256, (max_rows + BT_THREADS - 1) / BT_THREADS);
+    const int wgs = min(256, (max_rows - 1) / BT_THREADS + 1);
     hipLaunchKernelGGL(block_tables_kernel, dim3(wgs), dim3(BT_THREADS), 0, s, a);
     return hipGetLastError();
 }

@@ -1,0 +1,64 @@
+"""The paged 4-bit cache where its sizes end: caches of more than 4 GB, page numbers that no cache can have."""
+import numpy as np
+import pytest
+
+import paper_2409_11155_amd as iso      # first: binds libiso to the HIP runtime it was built against
+import iso_inputs
+from oracle import kv4_oracle as ko
+from test_gpu_kv4 import check, f64, ints, make_ctx
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dt,nq,d,kv,fresh", [("bf16", 8, 128, 600, 1), ("bf16", 8, 128, 600, 5), ("bf16", 64, 128, 700, 260), ("f32", 4, 128, 600, 2),
+                                              ("bf16", 16, 64, 500, 1), ("bf16", 64, 64, 600, 300)])
+def test_a_cache_of_more_than_4_GB(dt, nq, d, kv, fresh):
+    """Pages on both sides of the places where the codes' offsets pass 2^31 and 2^32 bytes, and the last one."""
+    page = 16
+    per_page = page * d // 2
+    ends = [2 ** 31 // per_page, 2 ** 32 // per_page]
+    n_pages = ends[1] + 100
+    need = -(-kv // page)
+    pages = np.unique(np.concatenate([[0, n_pages - 1]] + [np.arange(e - 6, e + 6) for e in ends] + [np.arange(need)]))[::-1][:need]
+    pages = np.random.default_rng(kv).permutation(pages).astype(np.int32)
+    assert len(pages) == need and {ends[0] - 1, ends[0], ends[1] - 1, ends[1], n_pages - 1} <= set(pages.tolist())
+    tok = np.arange(need * page)
+    slots = pages[tok // page] * page + tok % page
+    rng = np.random.default_rng(1)
+    k, v = (iso_inputs.store(rng.standard_normal((need * page, 1, d)).astype(np.float32), dt) for _ in range(2))
+    q = iso_inputs.randn((fresh, nq, d), seed=9, dtype=dt)
+    with make_ctx(nq, 1, d, dt) as ctx:
+        cache = ctx.kv4_cache(n_pages, page)
+        sd = ints(slots)
+        ctx.kv4_store(iso.DeviceArray.from_numpy(k, dt), iso.DeviceArray.from_numpy(v, dt), cache, sd, len(slots), ctx.stream0)
+        back = [iso.DeviceArray((len(slots), 1, d), dt, fill_byte=0xFF) for _ in range(2)]
+        ctx.kv4_load(cache, sd, back[0], back[1], len(slots), ctx.stream0)
+        out = iso.DeviceArray((fresh, nq, d), dt, fill_byte=0xFF)
+        n = ctx.attn_kv4_workspace(1, fresh)
+        ws = iso.DeviceArray((n,), "u8", fill_byte=0)
+        ctx.attn_kv4(iso.DeviceArray.from_numpy(q, dt), nq * d, cache, ints(pages), need, ints([0, fresh]), ints([kv]), 1, fresh, fresh, out, ws, n,
+                     ctx.stream0)
+        ctx.sync()
+        got, rows = f64(out, dt), [f64(b, dt) for b in back]
+    vals = [ko.decode(*ko.encode(f64(x, dt))) for x in (k, v)]
+    for r, w in zip(rows, vals):
+        np.testing.assert_array_equal(r, w)
+    kk, vv = (x.reshape(need, page, 1, d).transpose(0, 2, 1, 3) for x in vals)
+    check(got, f64(q, dt), kk, vv, np.arange(need, dtype=np.int32)[None], page, [0, fresh], [kv], nq, dt, need)
+
+
+def test_page_numbers_whose_slots_pass_31_bits_are_no_pages():
+    page, most = 64, 2 ** 31 // 64
+    free = np.array([most - 1, most, 2 ** 31 - 1, 5], np.int32)
+    table = np.array([[most, -9, -9], [most - 1, -9, -9]], np.int32)
+    with make_ctx(4, 4, 64, "f32") as ctx:
+        td, start, lens, pos, slots, nxt = (ints(a) for a in (table, [0] * 3, [0] * 2, [-5] * 200, [-5] * 200, [0]))
+        ctx.block_tables(ints([60, 62]), ints([100, 70]), 2, page, ints(free), 4, None, td, 3, start, lens, pos, slots, 200, nxt, ctx.stream0)
+        ctx.sync()
+        got = slots.numpy()
+    want = np.full(200, -1, np.int64)
+    p = np.arange(60, 160)
+    want[:100] = np.where(p // page == 1, (most - 1) * page + p % page, -1)
+    p = np.arange(62, 132)
+    want[100:170] = np.select([p // page == 0, p // page == 2], [(most - 1) * page + p % page, 5 * page + p % page], -1)
+    np.testing.assert_array_equal(got, want)
