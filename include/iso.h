@@ -320,6 +320,7 @@ int iso_gemm_fp8(iso_ctx *ctx, const void *a8, const float *sa, const void *w8, 
  *   bits.  Writing a block x: e = least integer with max|x| <= 7 * 2^e, not below -125 nor above 125; s = e + 127; each element the
  *   nearest of the values times 2^e, ties to the even code.  An element is off by at most 2^e, i.e. less than 2/7 of the block's
  *   largest.  A block with a NaN or an infinity gets s = 255 and stands for 32 NaN.
+ *   (Bytes 0, 1, 253 and 254 are not written, and what they stand for is not defined.)
  *   Layout.  k, v [n_pages, nkv, page, d/2] bytes; k_scale, v_scale [n_pages, nkv, page, d/32] bytes.  A token's slot is its page's
  *   number * page + its place in the page.  Both context types (ISO_F32, ISO_BF16) read and write it; nothing in it depends on the
  *   type.  The library never looks at a page that no table or slot names.
@@ -345,7 +346,7 @@ typedef struct {
  *   positions, slots [max_rows]  position and slot of every row; the slot is -1 where the request has no page (list too short,
  *                         table too narrow), both are -1 behind the last row.  Rows past max_rows are not written (row_start says how many
  *                         there are).
- * Outputs must not overlap inputs (ISO_ERR_SHAPE where kv_len is cached or fresh, or free_next is free_head).
+ * A page number whose slots would pass 31 bits counts as none.  Outputs must not overlap inputs or one another (ISO_ERR_SHAPE).
  * Errors: NULL, n_seqs outside [1, 4096], n_free < 0, max_pages < 1 or max_rows < 1, an unknown page size (ISO_ERR_SHAPE). */
 int iso_block_tables(iso_ctx *ctx, const int *cached, const int *fresh, int n_seqs, int page, const int *free_pages, int n_free,
                      const int *free_head, int *block_table, int max_pages, int *row_start, int *kv_len, int *positions, int *slots,
@@ -355,6 +356,7 @@ int iso_block_tables(iso_ctx *ctx, const int *cached, const int *fresh, int n_se
  * to slots[t].  The rotated q goes to q_out [T, nq, d], or back into qkv where q_out is NULL.  k is rotated in 64 bits (from the same
  * fp32 table), so that its codes are those of the exact value.  A row whose position is outside [0, max_seq) is left alone, q too; one
  * whose slot is not in the cache has only its q rotated.  Slots must differ from one another (else that slot's content is undefined).
+ * q_out must not overlap qkv (ISO_ERR_SHAPE).
  * Errors: NULL, T < 1, a cache that is none (ISO_ERR_SHAPE). */
 int iso_rope_kv4_write(iso_ctx *ctx, void *qkv, void *q_out, const iso_kv4 *cache, const int *positions, const int *slots, int T,
                        void *stream);
@@ -370,8 +372,9 @@ int iso_kv4_load(iso_ctx *ctx, const iso_kv4 *cache, const int *slots, void *k, 
  *   iso_attn_chunk.  A row that sees no key is zero.  Rows in front of the first request or behind the last are left as they were;
  *   what a cache holds in a token that a row does not see does not reach that row, NaN included.
  *   max_rows: the most rows that one request has, as far as known; the kernels are chosen by it, results are right for any value >= 1.
- *   ws: iso_attn_kv4_workspace bytes, zero-filled before its first use (every call leaves it ready for the next).  Calls that may
- *   overlap in time, replays of a graph among them, need one each.
+ *   ws: iso_attn_kv4_workspace bytes, zero-filled before its first use (every call leaves it ready for the next call of the same
+ *   context, of any shape that fits).  Calls that may overlap in time, replays of a graph among them, need one each.
+ *   q, out and ws must not overlap (ISO_ERR_SHAPE).
  * Results do not depend on the order in which workgroups run.
  * Errors: NULL, n_seqs outside [1, 4096], total_rows, max_rows or max_pages < 1, q_stride (ISO_ERR_SHAPE), ws too small
  * (ISO_ERR_WORKSPACE). */

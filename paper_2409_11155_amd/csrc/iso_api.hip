@@ -13,6 +13,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <vector>
 
 #include "iso_internal.h"
@@ -854,6 +855,18 @@ int run_split(iso_ctx *ctx, const iso_weights *layers, int n_layers, void *x, vo
 
 // ---- the paged 4-bit cache ---------------------------------------------------------------------
 bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+struct Bytes { const void *p; size_t n; };
+bool overlap(const Bytes &a, const Bytes &b) { return a.p && b.p && (uintptr_t)a.p < (uintptr_t)b.p + b.n && (uintptr_t)b.p < (uintptr_t)a.p + a.n; }
+// `outs` must overlap neither one another nor an input.
+int check_apart(std::initializer_list<Bytes> outs, std::initializer_list<Bytes> ins) {
+    for (const Bytes *o = outs.begin(); o != outs.end(); ++o) {
+        for (const Bytes *x = outs.begin(); x != o; ++x)
+            if (overlap(*o, *x)) return fail(ISO_ERR_SHAPE, "two outputs overlap");
+        for (const Bytes &x : ins)
+            if (overlap(*o, x)) return fail(ISO_ERR_SHAPE, "an output overlaps an input");
+    }
+    return ISO_OK;
+}
 bool page_size_known(int page) { return page >= 16 && page <= 256 && (page & (page - 1)) == 0; }
 
 // The kernels run where the stream is, and the launch goes to the current device.
@@ -1402,10 +1415,12 @@ int iso_block_tables(iso_ctx *ctx, const int *cached, const int *fresh, int n_se
     if (!page_size_known(page)) return fail(ISO_ERR_SHAPE, "page=%d must be 16, 32, 64, 128 or 256", page);
     if (n_free < 0 || max_pages < 1 || max_rows < 1)
         return fail(ISO_ERR_SHAPE, "n_free=%d must be >= 0, max_pages=%d and max_rows=%d positive", n_free, max_pages, max_rows);
-    if (kv_len == cached || kv_len == fresh || free_next == free_head) return fail(ISO_ERR_SHAPE, "outputs must not be inputs");
     const void *ints[] = {cached, fresh, free_pages, free_head, block_table, row_start, kv_len, positions, slots, free_next};
     for (const void *p : ints)
         if (!aligned(p, 4)) return fail(ISO_ERR_SHAPE, "int buffers must be 4-byte aligned");
+    const size_t seqs = 4 * (size_t)n_seqs, rows = 4 * (size_t)max_rows;
+    ISO_TRY(check_apart({{block_table, seqs * max_pages}, {row_start, seqs + 4}, {kv_len, seqs}, {positions, rows}, {slots, rows}, {free_next, 4}},
+                        {{cached, seqs}, {fresh, seqs}, {free_pages, 4 * (size_t)n_free}, {free_head, 4}}));
     ISO_TRY(check_device(ctx));
     LAUNCH_TRY(ISO_K_TABLES, (hipStream_t)stream,
                iso_launch_block_tables(cached, fresh, n_seqs, page, free_pages, n_free, free_head, block_table, max_pages, row_start, kv_len,
@@ -1421,8 +1436,10 @@ int iso_rope_kv4_write(iso_ctx *ctx, void *qkv, void *q_out, const iso_kv4 *cach
     ISO_TRY(check_rows(ctx->cfg, T));
     if (!aligned(qkv, 16) || !aligned(q_out, 16) || !aligned(positions, 4) || !aligned(slots, 4))
         return fail(ISO_ERR_SHAPE, "qkv and q_out must be 16-byte aligned, positions and slots 4-byte");
-    ISO_TRY(check_device(ctx));
     const iso_cfg &c = ctx->cfg;
+    const size_t head = (size_t)T * c.head_dim * (c.dtype == ISO_F32 ? 4 : 2);
+    ISO_TRY(check_apart({{q_out, head * c.n_q_heads}}, {{qkv, head * (c.n_q_heads + 2 * c.n_kv_heads)}}));
+    ISO_TRY(check_device(ctx));
     LAUNCH_TRY(ISO_K_ROPE_KV, (hipStream_t)stream,
                iso_launch_kv4_write(c.dtype, qkv, q_out, *cache, positions, slots, ctx->rope_cos, ctx->rope_sin, c.max_seq, T, c.n_q_heads,
                                     c.n_kv_heads, c.head_dim, (hipStream_t)stream), "rope+kv4");
@@ -1448,8 +1465,10 @@ int iso_kv4_load(iso_ctx *ctx, const iso_kv4 *cache, const int *slots, void *k, 
     ISO_TRY(check_kv4(cache));
     ISO_TRY(check_rows(ctx->cfg, T));
     if (!aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 4)) return fail(ISO_ERR_SHAPE, "k and v must be 16-byte aligned, slots 4-byte");
-    ISO_TRY(check_device(ctx));
     const iso_cfg &c = ctx->cfg;
+    const size_t bytes = (size_t)T * c.n_kv_heads * c.head_dim * (c.dtype == ISO_F32 ? 4 : 2);
+    ISO_TRY(check_apart({{k, bytes}, {v, bytes}}, {}));
+    ISO_TRY(check_device(ctx));
     LAUNCH_TRY(ISO_K_QUANT, (hipStream_t)stream,
                iso_launch_kv4_load(c.dtype, *cache, slots, k, v, T, c.n_kv_heads, c.head_dim, (hipStream_t)stream), "kv4 load");
     return ISO_OK;
@@ -1482,6 +1501,8 @@ int iso_attn_kv4(iso_ctx *ctx, const void *q, int q_stride, const iso_kv4 *cache
     if (ws_bytes < need) return fail(ISO_ERR_WORKSPACE, "ws of %zu bytes, %zu are needed", ws_bytes, need);
     if (!aligned(q, 16) || !aligned(out, 16) || !aligned(ws, 16) || !aligned(block_table, 4) || !aligned(row_start, 4) || !aligned(kv_len, 4))
         return fail(ISO_ERR_SHAPE, "q, out and ws must be 16-byte aligned, int buffers 4-byte");
+    const size_t elt = c.dtype == ISO_F32 ? 4 : 2, row = (size_t)c.n_q_heads * c.head_dim;
+    ISO_TRY(check_apart({{out, elt * total_rows * row}, {ws, need}}, {{q, elt * ((size_t)(total_rows - 1) * q_stride + row)}}));
     ISO_TRY(sk_status(ctx));
     ISO_TRY(check_device(ctx));
     const kv4_batch b{block_table, row_start, kv_len, max_pages, n_seqs, total_rows};

@@ -175,11 +175,11 @@ def kernels(dt, nq, nkv, d, n_seqs, rows, most):
     with iso.Context(iso.make_cfg(64, nq, nkv, d, 64, dt, 256)) as ctx:
         cache = ctx.kv4_cache(4, 16)
         i = iso.DeviceArray((64,), "i32")
-        q = iso.DeviceArray((rows, nq, d), dt)
+        q, out = (iso.DeviceArray((rows, nq, d), dt) for _ in range(2))
         n = ctx.attn_kv4_workspace(n_seqs, rows)
         ws = iso.DeviceArray((n,), "u8")
         log()
-        ctx.attn_kv4(q, nq * d, cache, i, 4, i, i, n_seqs, rows, most, q, ws, n)
+        ctx.attn_kv4(q, nq * d, cache, i, 4, i, i, n_seqs, rows, most, out, ws, n)
         return [l[2].split()[0] for l in log() if l[0] == "kernel"]
 def line(name, rt):
     return "attn_kv4_kernel" in name and name.split("Li")[-1].startswith(str(rt))
@@ -193,3 +193,48 @@ k = kernels("bf16", 8, 1, 128, 2, 4096, 2047); assert len(k) == 1 and line(k[0],
 k = kernels("bf16", 130, 1, 64, 1, 200, 200);  assert len(k) == 1 and line(k[0], 2), k
 k = kernels("f32", 8, 1, 128, 1, 4096, 4096);  assert len(k) == 1 and line(k[0], 1), k
 """)
+
+
+OVERLAPS = """
+L = iso.load()
+with iso.Context(iso.make_cfg(64, 4, 2, 64, 64, "bf16", 256)) as ctx:
+    h = ctx._h
+    cache = ctx.kv4_cache(4, 16)
+    def refuses(f, *a):
+        assert getattr(L, "iso_" + f)(h, *a, None) == -2, (f, a)
+        assert "overlap" in iso.last_error()
+    mem = iso.DeviceArray((1 << 16,), "u8").ptr                # places in one buffer; 8 rows of 8 heads are 8192 bytes
+    # lengths, free pages, table of 2 x 4, starts, lengths, positions, slots of 8 rows, next
+    at = {n: mem + 64 * i for i, n in enumerate("cached fresh free_pages head table start kv_len positions slots next".split())}
+    def tables(**kw):
+        p = {**at, **kw}
+        return (p["cached"], p["fresh"], 2, 16, p["free_pages"], 8, p["head"], p["table"], 4, p["start"], p["kv_len"], p["positions"], p["slots"], 8, p["next"])
+    assert L.iso_block_tables(h, *tables(), None) == 0, iso.last_error()
+    assert L.iso_block_tables(h, *tables(fresh=at["cached"], next=at["head"] + 4), None) == 0      # inputs may be one another
+    for kw in (dict(kv_len=at["cached"]), dict(kv_len=at["fresh"] + 4), dict(next=at["head"]), dict(table=at["free_pages"] + 28), dict(slots=at["positions"] + 28),
+               dict(start=at["kv_len"] - 8), dict(positions=at["cached"] - 28), dict(next=at["table"] + 28)):
+        refuses("block_tables", *tables(**kw))
+    ck = cache.ref
+    i = mem + 60000
+    assert L.iso_rope_kv4_write(h, mem, mem + 8192, ck, i, i, 8, None) == 0
+    for q in (mem, mem + 8192 - 16, mem + 4096):
+        refuses("rope_kv4_write", mem, q, ck, i, i, 8)
+    refuses("rope_kv4_write", mem + 4096, mem + 16, ck, i, i, 8)
+    assert L.iso_kv4_load(h, ck, i, mem, mem + 2048, 8, None) == 0
+    refuses("kv4_load", ck, i, mem, mem + 2032, 8)
+    assert L.iso_kv4_store(h, mem, mem, ck, i, 8, None) == 0    # inputs may be
+    n = ctx.attn_kv4_workspace(1, 8)
+    ws = iso.DeviceArray((n + 4096,), "u8").ptr
+    def attn(q, out, w):
+        return (q, 512, ck, i, 4, i, i, 1, 8, 8, out, w, n)
+    end = 7 * 1024 + 512                                       # of q: rows 512 elements apart, 256 of them read
+    assert L.iso_attn_kv4(h, *attn(mem, mem + end, ws), None) == 0, iso.last_error()
+    refuses("attn_kv4", *attn(mem, mem, ws))
+    refuses("attn_kv4", *attn(mem, mem + end - 16, ws))
+    refuses("attn_kv4", *attn(ws + n - 16, mem, ws))
+    refuses("attn_kv4", *attn(mem, ws, ws))
+"""
+
+
+def test_overlapping_buffers_are_refused(fake):                # noqa: F811
+    run(fake, OVERLAPS)
