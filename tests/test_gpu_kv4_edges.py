@@ -1,11 +1,12 @@
-"""The paged 4-bit cache where its sizes end: caches of more than 4 GB, page numbers that no cache can have."""
+"""The paged 4-bit cache where its sizes end: caches of more than 4 GB, page numbers that no cache can have, many heads, keys that are
+NaN, fewer rows than the requests have."""
 import numpy as np
 import pytest
 
 import paper_2409_11155_amd as iso      # first: binds libiso to the HIP runtime it was built against
 import iso_inputs
 from oracle import kv4_oracle as ko
-from test_gpu_kv4 import check, f64, ints, make_ctx
+from test_gpu_kv4 import FLAGS, attend, batch, check, device_cache, f64, fill, ints, make_ctx
 
 pytestmark = pytest.mark.gpu
 
@@ -62,3 +63,49 @@ def test_page_numbers_whose_slots_pass_31_bits_are_no_pages():
     p = np.arange(62, 132)
     want[100:170] = np.select([p // page == 0, p // page == 2], [(most - 1) * page + p % page, 5 * page + p % page], -1)
     np.testing.assert_array_equal(got, want)
+
+
+@pytest.mark.parametrize("nq,nkv,d", [(130, 1, 64), (200, 2, 64), (65, 1, 128)])
+@pytest.mark.parametrize("kv,fresh", [([70, 1, 500], [1, 1, 1]), ([300, 40], [260, 2])])
+def test_more_than_64_query_heads_of_a_key_head(nq, nkv, d, kv, fresh):
+    table, row_start, n_pages = batch(kv, fresh, 32, seed=1)
+    codes, scales = fill(n_pages, nkv, 32, d, 7, table, kv)
+    q = iso_inputs.randn((int(row_start[-1]), nq, d), seed=9, dtype="bf16")
+    with make_ctx(nq, nkv, d, "bf16") as ctx:
+        got = f64(attend(ctx, q, device_cache(codes, scales, 32), table, row_start, kv, "bf16", nq, d), "bf16")
+    check(got, f64(q, "bf16"), ko.decode(codes[0], scales[0]), ko.decode(codes[1], scales[1]), table, 32, row_start, kv, nq // nkv, "bf16", n_pages)
+
+
+@pytest.mark.parametrize("flags", FLAGS)
+@pytest.mark.parametrize("dt,nq,nkv,d", [("bf16", 8, 1, 128), ("bf16", 64, 1, 128), ("bf16", 64, 1, 64), ("f32", 4, 2, 64)])
+@pytest.mark.parametrize("kv,fresh,bad", [(900, 260, 700), (900, 1, 899), (700, 3, 698), (64, 64, 0)])
+def test_a_key_that_is_nan_reaches_the_rows_that_see_it_whole_and_no_others(dt, nq, nkv, d, kv, fresh, bad, flags):
+    page = 16
+    table, row_start, n_pages = batch([kv], [fresh], page, seed=5)
+    codes, scales = fill(n_pages, nkv, page, d, 6, table, [kv])
+    clean = scales[0].copy()
+    scales[0][table[0, bad // page], :, bad % page, 0] = 255
+    q = iso_inputs.randn((fresh, nq, d), seed=4, dtype=dt)
+    with make_ctx(nq, nkv, d, dt) as ctx:
+        ctx.set_flags(flags)
+        got = f64(attend(ctx, q, device_cache(codes, scales, page), table, row_start, [kv], dt, nq, d), dt)
+    sees = max(0, bad - (kv - fresh))
+    assert np.isnan(got[sees:]).all() and not np.isnan(got[:sees]).any()
+    if sees:
+        k, v = ko.decode(codes[0], clean), ko.decode(codes[1], scales[1])
+        ref = ko.attention(f64(q, dt), k, v, table, page, row_start, [kv], nq // nkv, n_pages)[0]
+        check(np.concatenate((got[:sees], ref[sees:])), f64(q, dt), k, v, table, page, row_start, [kv], nq // nkv, dt, n_pages)
+
+
+@pytest.mark.parametrize("flags", FLAGS)
+@pytest.mark.parametrize("dt,nq,nkv,d", [("bf16", 8, 1, 128), ("bf16", 64, 1, 128), ("f32", 4, 2, 64)])
+def test_rows_past_the_last_that_the_call_has(dt, nq, nkv, d, flags):
+    """row_start ends at 420, the call has 300 rows: the second request's are cut, the third has none; the others are as ever."""
+    kv, fresh, page, rows = [500, 333, 90], [257, 120, 43], 32, 300
+    table, row_start, n_pages = batch(kv, fresh, page, seed=3)
+    codes, scales = fill(n_pages, nkv, page, d, 6, table, kv)
+    q = iso_inputs.randn((rows, nq, d), seed=4, dtype=dt)
+    with make_ctx(nq, nkv, d, dt) as ctx:
+        ctx.set_flags(flags)
+        got = f64(attend(ctx, q, device_cache(codes, scales, page), table, row_start, kv, dt, nq, d), dt)
+    check(got, f64(q, dt), ko.decode(codes[0], scales[0]), ko.decode(codes[1], scales[1]), table, page, row_start, kv, nq // nkv, dt, n_pages)
