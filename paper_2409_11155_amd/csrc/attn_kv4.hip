@@ -31,12 +31,12 @@ typedef __bf16 bf16x4_v __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2_v __attribute__((ext_vector_type(2)));
 
 constexpr int WAVES = 4, THREADS = 64 * WAVES, TILE = 32, UNIT = WAVES * TILE;
-constexpr int GROUP = 16;                // pieces that are folded at once; a tile has up to GROUP * GROUP of them
+constexpr int GROUP = 16;             // pieces that are folded at once, at most; a tile has up to GROUP * GROUP of them
 constexpr int SETUP = 512;            // what a tile's start and end cost, in keys
 constexpr int ROUND = 256;            // keys that cost what a second round of folding does: 18 rows, 7300 keys each, 22.4 us with two, 17.1 with one
-constexpr int MIN_SHARE = 256;         // keys of a share, at least
-constexpr int COHERENT = 1 | 16;         // buffer cache policy sc0 | sc1: system scope, bypasses the XCD-local L2
-constexpr int SPLITS = GROUP * GROUP - 2;      // shares that the longest tile is cut into, at most (a share may begin and end inside it)
+constexpr int MIN_SHARE = 256;        // keys of a share, at least
+constexpr int COHERENT = 1 | 16;      // buffer cache policy sc0 | sc1: system scope, bypasses the XCD-local L2
+constexpr int SPLITS = GROUP * GROUP - 2;  // shares that the longest tile is cut into, at most (a share may begin and end inside it)
 
 // Workgroups on a compute unit, by the registers.
 constexpr int wg_per_cu(int elt, int d, int rt) { return elt == 4 ? (d == 64 ? 3 : 2) : rt == 2 ? (d == 64 ? 3 : 2) : d == 64 ? 4 : 3; }
@@ -50,6 +50,7 @@ struct line_args {
     kv4_view c;
     kv4_batch b;
     int q_stride, nq, nkv, G;            // G: query heads of a key head
+    unsigned g_mul, g_bits;              // x / G = (x * g_mul / 2^32 + x) >> g_bits for x below 2^31
     int most;                            // requests of more (row, head) pairs than this belong to another launch
 };
 
@@ -88,26 +89,38 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t beyond(unsigned char *p, uint6
 __device__ __forceinline__ scalar_ints scalar(const int *p) { return (scalar_ints)(uintptr_t)p; }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ u64 uniform(u64 x) { return (u64)(unsigned)uniform((int)x) | (u64)(unsigned)uniform((int)(x >> 32)) << 32; }
-// x / d for quotients below 2^24, with inv about 1 / d (the instruction gives 2^-26 or better): off by one at most before it is set right.
-__device__ __forceinline__ int quotient(u64 x, u64 d, double inv) {
-    const int q = (int)((double)x * inv);
-    const u64 p = (u64)(long long)q * d;
+// x / d, with inv about 1 / d: the estimate is off by one at most (quotients below 2^20 in 32 bits, below 2^24 in 64) before it is set right.
+template <typename F> __device__ __forceinline__ int quotient(u64 x, u64 d, F inv) {
+    const int q = (int)((F)x * inv);
+    const u64 p = (u64)(unsigned)q * d;
     return uniform(x < p ? q - 1 : x - p >= d ? q + 1 : q);
 }
 
-// Inclusive sum and maximum over the wave, lane 63 holds all of it: row shifts, then the last lanes of the rows handed on (DPP, no LDS).
+// Inclusive sum over the wave and its maximum, lane 63 holds all of it: row shifts, then the last lanes of the rows handed on (DPP, no LDS).
 template <int CTRL, int ROW_MASK> __device__ __forceinline__ u64 moved(u64 x) {
     const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROW_MASK, 0xf, false);
     const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(x >> 32), CTRL, ROW_MASK, 0xf, false);
     return (u64)hi << 32 | lo;
 }
-template <typename F> __device__ __forceinline__ u64 wave_scan(u64 x, F f) {
-    x = f(x, moved<0x111, 0xf>(x));
-    x = f(x, moved<0x112, 0xf>(x));
-    x = f(x, moved<0x114, 0xf>(x));
-    x = f(x, moved<0x118, 0xf>(x));
-    x = f(x, moved<0x142, 0xa>(x));
-    return f(x, moved<0x143, 0xc>(x));
+__device__ __forceinline__ u64 wave_scan(u64 x) {
+    x += moved<0x111, 0xf>(x);
+    x += moved<0x112, 0xf>(x);
+    x += moved<0x114, 0xf>(x);
+    x += moved<0x118, 0xf>(x);
+    x += moved<0x142, 0xa>(x);
+    return x + moved<0x143, 0xc>(x);
+}
+template <int CTRL, int ROW_MASK> __device__ __forceinline__ float moved(float x) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, ROW_MASK, 0xf, false));
+}
+__device__ __forceinline__ float wave_max(float x) {           // of numbers >= 0
+    x = fmaxf(x, moved<0x111, 0xf>(x));
+    x = fmaxf(x, moved<0x112, 0xf>(x));
+    x = fmaxf(x, moved<0x114, 0xf>(x));
+    x = fmaxf(x, moved<0x118, 0xf>(x));
+    x = fmaxf(x, moved<0x142, 0xa>(x));
+    x = fmaxf(x, moved<0x143, 0xc>(x));
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 __device__ __forceinline__ u64 lane_of(u64 x, int lane) {
     return (u64)(unsigned)__builtin_amdgcn_readlane((int)x, lane) | (u64)(unsigned)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32;
@@ -129,6 +142,7 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
     const int wave = uniform(tid >> 6);
     const kv4_batch &b = a.b;
     const int shift = a.c.page_shift, G = a.G, kvh = blockIdx.y;
+    auto by_g = [&](int x) { return (int)((__umulhi((unsigned)x, a.g_mul) + (unsigned)x) >> a.g_bits); };
 
     // ---- the line: places in front of every request, and in all.  Every wave does this for itself, 64 requests at a time: no barrier,
     // and for up to 64 of them one trip to memory.
@@ -140,32 +154,36 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
     };
     auto places = [](const Req &q, unsigned k) { return k * q.start + (u64)ROWS * ((u64)k * (k + 1) / 2); };      // of the first k tiles
     auto of_lane = [&](int i) { return i < b.n_seqs ? places(request(i), request(i).tiles) : 0; };
-    auto add = [](u64 x, u64 y) { return x + y; };
-    u64 mine = 0, longest = 0;
+    u64 mine = 0;
+    float longest = 0.f;
+    Req here;                                    // of the lane, where there are no more than 64 requests
     for (int i0 = 0; i0 < b.n_seqs; i0 += 64) {
         const int i = min(i0 + lane, b.n_seqs - 1);
-        const Req q = request(i);
-        if (i == i0 + lane) mine += places(q, q.tiles);
-        if (q.tiles) longest = max(longest, q.start + (u64)ROWS * q.tiles);
+        here = request(i);
+        if (i == i0 + lane) mine += places(here, here.tiles);
+        if (here.tiles) longest = fmaxf(longest, (float)here.start + (float)ROWS * (float)here.tiles);
     }
-    u64 incl = wave_scan(mine, add);
+    u64 incl = wave_scan(mine);
     const u64 all = lane_of(incl, 63);
-    longest = lane_of(wave_scan(longest, [](u64 x, u64 y) { return max(x, y); }), 63);
-    // any share does that covers the line; never less than MIN_SHARE keys, nor so little that a tile has more pieces than can be folded
-    u64 per = max(max((u64)((double)all * (1.000001 * __builtin_amdgcn_rcp((double)gridDim.x))) + 1, (u64)((double)longest * (1.0 / SPLITS)) + 1),
-                  (u64)G * MIN_SHARE);
+    longest = wave_max(longest);
+    // Any share does that covers the line (2^-17 more than its part, for the roundings); never less than MIN_SHARE keys, nor so little that
+    // a tile has more pieces than can be folded.
+    constexpr float MORE = 1.f + 0x1p-17f;
+    float share = fmaxf(fmaxf((float)all * (MORE * __builtin_amdgcn_rcpf((float)gridDim.x)), longest * (MORE / SPLITS)), (float)(G * MIN_SHARE));
     // one round of folding instead of two where that lengthens a share by less than ROUND keys
-    const u64 one_round = (u64)((double)longest * (1.0 / (GROUP - 1))) + 1;
-    if (one_round > per && one_round - per < (u64)G * ROUND) per = one_round;
+    const float one_round = longest * (MORE / (GROUP - 1));
+    if (one_round > share && one_round - share < (float)(G * ROUND)) share = one_round;
+    u64 per = (u64)share + 1;
     per = uniform(per);
     u64 at = (u64)blockIdx.x * per;
     const u64 end = min(all, at + per);
     if (at >= end) return;
-    const double inv_per = __builtin_amdgcn_rcp((double)per), inv_unit = __builtin_amdgcn_rcp((double)(UNIT * G));
+    const float inv_per = __builtin_amdgcn_rcpf((float)per);
+    const double inv_unit = __builtin_amdgcn_rcp((double)(UNIT * G));
     int seq = 0;
     u64 inside = at;                             // place inside the request
     for (int i0 = 0;; i0 += 64) {
-        if (b.n_seqs > 64) incl = wave_scan(of_lane(i0 + lane), add);
+        if (b.n_seqs > 64) incl = wave_scan(of_lane(i0 + lane));
         const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(incl <= inside));      // requests that end before it
         if (n < 64) {
             seq = i0 + n;
@@ -185,13 +203,20 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
     const int out_row = 4 * g4 + (n16 >> 2);
     const unsigned v_out = lds_w + out_row * RB + ((((n16 & 3) >> 1) ^ swz(out_row)) << 4) + ((n16 & 1) << 3);
 
+    // (what a lane has read already is not read again: a trip to memory)
+    Req rq;
+    if (b.n_seqs <= 64) {
+        auto of = [&](int x) { return __builtin_amdgcn_readlane(x, seq); };
+        rq = Req{of(here.first), of(here.n), of(here.base), of(here.keys), (unsigned)of((int)here.tiles), lane_of(here.start, seq)};
+    } else {
+        rq = request(seq);
+    }
     for (;;) {
-        const Req rq = request(seq);
         // ---- the tile that place `inside` lies in: the largest k with places(k) <= inside
         unsigned tile = 0;
         if (rq.tiles > 1) {
-            const double c = ((double)rq.start + 0.5 * ROWS) * (1.0 / ROWS);
-            tile = min(rq.tiles - 1, (unsigned)max(0.0, sqrt(c * c + (2.0 / ROWS) * (double)inside) - c));
+            const float c = ((float)rq.start + 0.5f * ROWS) * (1.f / ROWS), x = (2.f / ROWS) * (float)inside;      // root of k^2 + 2 c k = x
+            tile = min(rq.tiles - 1, (unsigned)(x * __builtin_amdgcn_rcpf(c + __builtin_amdgcn_sqrtf(c * c + x))));
             while (tile > 0 && places(rq, tile) > inside) --tile;
             while (tile + 1 < rq.tiles && places(rq, tile + 1) <= inside) ++tile;
             tile = (unsigned)uniform((int)tile);
@@ -201,7 +226,7 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
         const int pairs = rq.n * G, first_pair = (int)tile * ROWS;
         const bool two = RT == 2 && pairs - first_pair > 16;
         auto limit = [&](int tok) { return (int)max(0ll, min((long long)rq.keys, (long long)rq.base + tok + 1)); };      // keys that a token sees
-        const int lim_lo = uniform(limit(first_pair / G)), lim_hi = uniform(limit((min(pairs, first_pair + ROWS) - 1) / G));
+        const int lim_lo = uniform(limit(by_g(first_pair))), lim_hi = uniform(limit(by_g(min(pairs, first_pair + ROWS) - 1)));
         // ---- the piece's keys (the share begins and ends at multiples of UNIT keys of the tile), and the workgroups that have pieces
         const u64 s_keys = s0 + (u64)G * SETUP;
         auto key_at = [&](u64 place) { return place < s_keys ? 0 : quotient(place - s_keys, (u64)G * UNIT, inv_unit) * UNIT; };
@@ -217,7 +242,7 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
             float m_run[RT], l_run[RT];                // maximum in units of the base-2 exponent
 #pragma unroll
             for (int x = 0; x < RT; ++x) {
-                const int r = first_pair + 16 * x + n16, t = r / G, head = kvh * G + (r - t * G);
+                const int r = first_pair + 16 * x + n16, t = by_g(r), head = kvh * G + (r - t * G);
                 real[x] = r < pairs;
                 lim[x] = real[x] ? limit(t) : lim_lo;
                 const T *qp = (const T *)a.q + (size_t)(rq.first + (real[x] ? t : 0)) * a.q_stride + (size_t)(real[x] ? head : 0) * D + g4 * WPL * 8;
@@ -292,6 +317,8 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
                     }
                 }
                 f32x4_t s[RT][2];
+                // unpacking and scores go before the other workgroups' softmax: 64 rows x 16 heads over 32768 keys 49.6 -> 47.1 us
+                __builtin_amdgcn_s_setprio(1);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -323,6 +350,7 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
                     }
                 };
                 read_v(0, 0);
+                __builtin_amdgcn_s_setprio(0);
                 __builtin_amdgcn_sched_barrier(0);
                 float mx[RT];
                 bool moves = false;
@@ -456,9 +484,10 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
             const int rows = min(ROWS, pairs - first_pair);
             bool writes = true;
             if (w1 > w0) {
-                // ---- a piece of the tile: park it; the last to arrive of sixteen neighbours folds theirs, and where there are more than
-                // sixteen, the last of the groups folds the groups'.  (One workgroup reading 126 pieces of 4 KB took 13 us: a trip to
-                // memory for every 64 KB that four waves can have on their way.)
+                // ---- a piece of the tile: park it.  Up to GROUP pieces are folded by the workgroup that arrives last.  More of them go in
+                // groups of about their number's root, 8 or 16: the last to arrive of a group folds it, the last of those the groups'.  (A
+                // compute unit gets about 45 GB/s of pieces from memory: 126 of 4 KB took one workgroup 13 us.  16 rows, 16 heads over 2,
+                // 8192 keys, pieces of 16 KB: 25.7 us with groups of 16, 22.4 with smaller ones.)
                 constexpr int SLOT = slot_floats(D, RT) * 4;
                 const __amdgpu_buffer_rsrc_t rp = __builtin_amdgcn_make_buffer_rsrc((char *)a.part + (size_t)kvh * gridDim.x * 2 * SLOT, 0, (int)(gridDim.x * 2 * SLOT), 0x00020000);
                 auto index = [&](int w) { return 2 * w + (w == w0 ? 1 : 0); };      // a workgroup's tile from before, or the one begun here
@@ -533,15 +562,16 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
                     }
                 };
                 unsigned *const cnt = a.cnt + (size_t)kvh * gridDim.x * 3;     // two of pieces and one of groups a workgroup
-                const int n = w1 - w0 + 1, group = ((int)blockIdx.x - w0) / GROUP, head = w0 + group * GROUP, groups = (n + GROUP - 1) / GROUP;
+                const int n = w1 - w0 + 1, bits = n <= GROUP || n > GROUP * GROUP / 4 ? 4 : 3, size = 1 << bits;
+                const int group = ((int)blockIdx.x - w0) >> bits, head = w0 + (group << bits), groups = (n + size - 1) >> bits, members = min(size, n - (group << bits));
                 park(blockIdx.x);
-                writes = last_of(cnt + index(head), min(GROUP, n - group * GROUP));
+                writes = last_of(cnt + index(head), members);
                 if (writes) {
-                    fold(head, 1, min(GROUP, n - group * GROUP));
+                    fold(head, 1, members);
                     if (groups > 1) {
                         park(head);                      // in the place of the group's first piece, which is read
                         writes = last_of(cnt + 2 * gridDim.x + w0, groups);
-                        if (writes) fold(w0, GROUP, groups);
+                        if (writes) fold(w0, size, groups);
                     }
                 }
             }
@@ -549,7 +579,7 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
 #pragma unroll
                 for (int x = 0; x < RT; ++x)
                     if (16 * x + row < rows) {
-                        const int rr = first_pair + 16 * x + row, tok = rr / G;
+                        const int rr = first_pair + 16 * x + row, tok = by_g(rr);
                         const float inv = l[x] == 0.f ? 0.f : 1.0f / l[x];
                         T *op = (T *)a.out + ((size_t)(rq.first + tok) * a.nq + kvh * G + (rr - tok * G)) * D + col * CPT * 4;
 #pragma unroll
@@ -568,7 +598,8 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
             inside = 0;
             do {
                 seq = uniform(seq + 1);
-            } while (request(seq).tiles == 0);
+                rq = request(seq);
+            } while (rq.tiles == 0);
         }
     }
 }
@@ -599,7 +630,9 @@ size_t iso_attn_kv4_ws_bytes(int dtype, int nkv, int d, int ncu) {
 
 hipError_t iso_launch_attn_kv4(int dtype, const void *q, int q_stride, const iso_kv4 &cache, const kv4_batch &b, int max_rows, int most, void *out,
                                int nq, int nkv, int d, void *ws, hipStream_t s) {
-    const line_args a{q, out, nullptr, nullptr, kv4_view_of(cache), b, q_stride, nq, nkv, nq / nkv, most};
+    const unsigned G = (unsigned)(nq / nkv), bits = G == 1 ? 0 : 32 - __builtin_clz(G - 1);        // 2^bits >= G
+    const unsigned mul = (unsigned)(((((u64)1 << bits) - G) << 32) / G) + 1;
+    const line_args a{q, out, nullptr, nullptr, kv4_view_of(cache), b, q_stride, nq, nkv, (int)G, mul, bits, most};
     const bool two = std::min((long long)max_rows * a.G, (long long)most) > 16;
     if (dtype == ISO_F32) return d == 64 ? launch<float, 64, 1>(a, ws, s) : launch<float, 128, 1>(a, ws, s);
     if (d == 64) return two ? launch<bf16_t, 64, 2>(a, ws, s) : launch<bf16_t, 64, 1>(a, ws, s);
