@@ -633,7 +633,12 @@ hipError_t iso_launch_attn_kv4(int dtype, const void *q, int q_stride, const iso
     const unsigned G = (unsigned)(nq / nkv), bits = G == 1 ? 0 : 32 - __builtin_clz(G - 1);        // 2^bits >= G
     const unsigned mul = (unsigned)(((((u64)1 << bits) - G) << 32) / G) + 1;
     const line_args a{q, out, nullptr, nullptr, kv4_view_of(cache), b, q_stride, nq, nkv, (int)G, mul, bits, most};
-    const bool two = std::min((long long)max_rows * a.G, (long long)most) > 16;
+    // Two blocks of rows a tile where a request can have more than one, and, with heads of 128 (two workgroups on a compute unit then instead
+    // of three, pieces twice as large), where a workgroup's share is about 1024 keys or more by the room that the table has.  16 and 32
+    // rows a tile, 16 heads over 2: 5 rows for each of 8 requests of up to 4000 keys 14 and 22 us; 509 rows of 700 / 2048 / 6000 17 / 30 / 62 and
+    // 19 / 28 / 54; heads of 64, 32 over 8: 200 rows of 2048 23 and 20, 500 of 500 19 and 16.
+    const long long keys = std::min((long long)b.max_pages * cache.page, 0x7fffffffll), pairs = (long long)b.total_rows * nq;
+    const bool two = std::min((long long)max_rows * a.G, (long long)most) > 16 && (d == 64 || pairs / 32 * keys >= 1024ll * wg_per_cu(2, 128, 2) * iso_num_cu());
     if (dtype == ISO_F32) return d == 64 ? launch<float, 64, 1>(a, ws, s) : launch<float, 128, 1>(a, ws, s);
     if (d == 64) return two ? launch<bf16_t, 64, 2>(a, ws, s) : launch<bf16_t, 64, 1>(a, ws, s);
     return two ? launch<bf16_t, 128, 2>(a, ws, s) : launch<bf16_t, 128, 1>(a, ws, s);

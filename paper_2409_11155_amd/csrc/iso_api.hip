@@ -895,21 +895,27 @@ int check_kv4(const iso_kv4 *c) {
     return ISO_OK;
 }
 
-// Which kernels a batch needs, and their regions of its workspace (both are there whatever max_rows says).  Long chunks go to the tiles
-// of 128 rows: 8 heads, 2048 rows over 2048 / 8192 / 32768 keys 33 / 93 / 350 us, with 32 rows a tile 35 / 119 / 440; 16 heads, 1024 rows over 6000
-// keys 78 and 98; but 509 over 700 keys 39 and 21, 16 over 8192 47 and 26: they need many row tiles.  Shorter requests of such a batch
-// stay with the other kernel, which costs a second launch.
+// Which kernels a batch needs, and their regions of its workspace (both are there whatever the call's max_rows and table).  Long chunks
+// deep in a cache go to the tiles of 128 rows, everything else to the line of 16 or 32 rows a tile.  What there is to do is taken to be
+// (row, head) pairs times the keys that the table has room for.  One request (us, tiles of 128 rows and the line):
+//   16 heads over 2:  512 rows of 2048 / 4096 / 32768 keys   36 / 44 / 169 and 28 / 42 / 209;  2000 of 2000  41 and 50
+//                     128 / 256 rows of 32768                85 / 98 and 68 / 115;             16 of 8192    47 and 20
+//   8 heads over 1:   2048 rows of 2048 / 8192 / 32768       34 / 86 / 321 and 33 / 111 / 416
+//   13 heads over 13: 640 rows of 2048 / 4096, 2047 of 2047  34 / 42 / 38 and 28 / 41 / 45
+// Of several requests the shorter ones stay with the line, which costs a second launch: 22 single tokens (16 heads over 2) and
+//   2 x 512 rows of up to 6000 / 20000 keys  59 / 109 and 51 / 117;  4 x 512 of up to 8192  103 and 116;  1024 of up to 6000  49 and 35
 struct Kv4Launch {
     bool line, rows;
     int most;                      // pairs of (row, query head of a key head) up to which a request belongs to the line
     size_t line_bytes, rows_bytes;
 };
-Kv4Launch kv4_launch(const iso_cfg &c, int n_seqs, int total_rows, int max_rows) {
+Kv4Launch kv4_launch(const iso_cfg &c, int n_seqs, int total_rows, int max_rows, long long keys) {
     const int ncu = iso_num_cu();
     const bool can = c.dtype == ISO_BF16 && c.n_q_heads / c.n_kv_heads <= 64;
-    auto many = [&](int rows) { return can && (long long)rows * c.n_q_heads >= 16384; };
+    auto many = [&](int rows) { return can && (long long)rows * c.n_q_heads >= 4096; };
+    const long long work = (long long)total_rows * c.n_q_heads * std::min(keys, 0x7fffffffll);
     Kv4Launch l;
-    l.rows = many(n_seqs == 1 ? total_rows : std::min(max_rows, total_rows));
+    l.rows = n_seqs == 1 ? many(total_rows) && work > 1ll << 25 : many(std::min(max_rows, total_rows)) && work > 1ll << 27;
     l.line = !l.rows || n_seqs > 1;
     l.most = !l.rows ? 0x7fffffff : l.line ? 1023 : 0;
     l.line_bytes = align_up(iso_attn_kv4_ws_bytes(c.dtype, c.n_kv_heads, c.head_dim, ncu), 256);
@@ -1480,7 +1486,7 @@ int iso_attn_kv4_workspace(iso_ctx *ctx, int n_seqs, int total_rows, size_t *byt
     if (total_rows < 1) return fail(ISO_ERR_SHAPE, "total_rows=%d must be positive", total_rows);
     if ((long long)total_rows * ctx->cfg.n_q_heads >= (1ll << 31))
         return fail(ISO_ERR_SHAPE, "total_rows=%d of %d heads: fewer than 2^31 together", total_rows, ctx->cfg.n_q_heads);
-    const Kv4Launch l = kv4_launch(ctx->cfg, n_seqs, total_rows, total_rows);
+    const Kv4Launch l = kv4_launch(ctx->cfg, n_seqs, total_rows, total_rows, 0);
     *bytes = l.line_bytes + l.rows_bytes;
     return ISO_OK;
 }
@@ -1512,7 +1518,7 @@ int iso_attn_kv4(iso_ctx *ctx, const void *q, int q_stride, const iso_kv4 *cache
                    "kv4 attention");
         return ISO_OK;
     }
-    const Kv4Launch l = kv4_launch(c, n_seqs, total_rows, max_rows);
+    const Kv4Launch l = kv4_launch(c, n_seqs, total_rows, max_rows, (long long)max_pages * cache->page);
     if (l.line)
         LAUNCH_TRY(ISO_K_ATTN, s, iso_launch_attn_kv4(c.dtype, q, q_stride, *cache, b, std::min(max_rows, total_rows), l.most, out, c.n_q_heads,
                                                       c.n_kv_heads, c.head_dim, ws, s), "kv4 attention");

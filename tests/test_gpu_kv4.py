@@ -182,6 +182,11 @@ def batch(kv, fresh, page, seed, spare=3):
     return table, np.concatenate(([0], np.cumsum(fresh))).astype(np.int32), n_pages
 
 
+def wide(table, page, keys):
+    """The table with room for `keys` tokens a request: kernels are chosen by it."""
+    return np.pad(table, ((0, 0), (0, max(0, keys // page - table.shape[1]))))
+
+
 def fill(n_pages, nkv, page, d, seed, table=None, kv=None):
     """Codes and scales of normal values in every place that a token has, NaN scales (and codes of six) everywhere else."""
     rng = np.random.default_rng(seed)
@@ -263,6 +268,21 @@ def test_attention(dt, heads, name, flags):
         assert (got[ref == 0] == 0).all() and (ref[0] == 0).all()
 
 
+@pytest.mark.parametrize("name", BATCHES)
+@pytest.mark.parametrize("heads", HEADS)
+def test_attention_through_a_table_with_room_for_more(heads, name):
+    """What much work would be done by: 32 rows a tile, 128 for the longest chunks."""
+    nq, nkv, d = heads
+    kv, fresh, page = BATCHES[name]
+    table, row_start, n_pages = batch(kv, fresh, page, seed=len(name))
+    table = wide(table, page, 1 << 20)
+    codes, scales = fill(n_pages, nkv, page, d, 7, table, kv)
+    q = iso_inputs.randn((int(row_start[-1]), nq, d), seed=9, dtype="bf16")
+    with make_ctx(nq, nkv, d, "bf16") as ctx:
+        got = f64(attend(ctx, q, device_cache(codes, scales, page), table, row_start, kv, "bf16", nq, d), "bf16")
+    check(got, f64(q, "bf16"), ko.decode(codes[0], scales[0]), ko.decode(codes[1], scales[1]), table, page, row_start, kv, nq // nkv, "bf16", n_pages)
+
+
 @pytest.mark.parametrize("flags", FLAGS)
 @pytest.mark.parametrize("dt,heads", [("bf16", (8, 1, 128)), ("bf16", (8, 8, 64)), ("f32", (4, 2, 64))])
 @pytest.mark.parametrize("max_rows", [1, 7, 1000])
@@ -317,7 +337,7 @@ def test_a_token_that_holds_nan_reaches_only_the_rows_that_see_it(dt, heads, fla
 
 # ------------------------------------------------------------------------------------------------ long chunks: tiles of 128 rows
 
-# rows x query heads from 16384 on: head layouts with many heads reach it with few rows
+# rows x query heads from 4096 on, and tables with room for many keys: head layouts with many heads reach it with few rows
 MANY = [(64, 1, 64), (64, 64, 64), (64, 2, 128), (66, 22, 128), (104, 8, 64)]
 LONG = {
     "fresh": ([256], [256], 64),
@@ -334,6 +354,7 @@ def test_long_chunks(heads, name):
     nq, nkv, d = heads
     kv, fresh, page = LONG[name]
     table, row_start, n_pages = batch(kv, fresh, page, seed=len(name))
+    table = wide(table, page, 8192)
     codes, scales = fill(n_pages, nkv, page, d, 7, table, kv)
     q = iso_inputs.randn((int(row_start[-1]), nq, d), seed=9, dtype="bf16")
     with make_ctx(nq, nkv, d, "bf16") as ctx:
@@ -353,7 +374,7 @@ def test_long_chunks_with_a_nan_and_missing_pages(heads, kv, fresh, bad):
     nq, nkv, d = heads
     page = 16
     table, row_start, n_pages = batch([kv], [fresh], page, seed=5)
-    row_start = row_start + 1
+    table, row_start = wide(table, page, 8192), row_start + 1
     gone = [2, 9] if kv > 300 else [5]
     table[0, gone] = [-1, n_pages][: len(gone)]
     codes, scales = fill(n_pages, nkv, page, d, 6, table, [kv])
@@ -374,12 +395,14 @@ def test_long_chunks_with_a_nan_and_missing_pages(heads, kv, fresh, bad):
 
 
 @pytest.mark.parametrize("dt,heads", [("bf16", (8, 1, 128)), ("bf16", (3, 3, 128)), ("bf16", (16, 4, 64)), ("f32", (4, 2, 64))])
+@pytest.mark.parametrize("room", [0, 1 << 20])
 @pytest.mark.parametrize("kv,fresh", [([40000], [1]), ([9000, 3, 20011], [1, 1, 6]), ([900] * 33, [1] * 33)])
-def test_many_pieces_and_one_workspace_for_all(dt, heads, kv, fresh):
+def test_many_pieces_and_one_workspace_for_all(dt, heads, kv, fresh, room):
     """Keys dealt to hundreds of workgroups and folded in two rounds; calls of other shapes on the same workspace in between."""
     nq, nkv, d = heads
     page = 64
     table, row_start, n_pages = batch(kv, fresh, page, seed=2)
+    table = wide(table, page, room)
     codes, scales = fill(n_pages, nkv, page, d, 3, table, kv)
     q = iso_inputs.randn((int(row_start[-1]), nq, d), seed=9, dtype=dt)
     other = batch([300, 77], [40, 1], page, seed=4)

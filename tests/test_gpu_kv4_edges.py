@@ -6,7 +6,7 @@ import pytest
 import paper_2409_11155_amd as iso      # first: binds libiso to the HIP runtime it was built against
 import iso_inputs
 from oracle import kv4_oracle as ko
-from test_gpu_kv4 import FLAGS, attend, batch, check, device_cache, f64, fill, ints, make_ctx
+from test_gpu_kv4 import FLAGS, attend, batch, check, device_cache, f64, fill, ints, make_ctx, wide
 
 pytestmark = pytest.mark.gpu
 
@@ -37,7 +37,7 @@ def test_a_cache_of_more_than_4_GB(dt, nq, d, kv, fresh):
         out = iso.DeviceArray((fresh, nq, d), dt, fill_byte=0xFF)
         n = ctx.attn_kv4_workspace(1, fresh)
         ws = iso.DeviceArray((n,), "u8", fill_byte=0)
-        ctx.attn_kv4(iso.DeviceArray.from_numpy(q, dt), nq * d, cache, ints(pages), need, ints([0, fresh]), ints([kv]), 1, fresh, fresh, out, ws, n,
+        ctx.attn_kv4(iso.DeviceArray.from_numpy(q, dt), nq * d, cache, ints(wide(pages[None], page, 1 << 20)), (1 << 20) // page, ints([0, fresh]), ints([kv]), 1, fresh, fresh, out, ws, n,
                      ctx.stream0)
         ctx.sync()
         got, rows = f64(out, dt), [f64(b, dt) for b in back]
@@ -82,6 +82,7 @@ def test_more_than_64_query_heads_of_a_key_head(nq, nkv, d, kv, fresh):
 def test_a_key_that_is_nan_reaches_the_rows_that_see_it_whole_and_no_others(dt, nq, nkv, d, kv, fresh, bad, flags):
     page = 16
     table, row_start, n_pages = batch([kv], [fresh], page, seed=5)
+    table = wide(table, page, 8192)
     codes, scales = fill(n_pages, nkv, page, d, 6, table, [kv])
     clean = scales[0].copy()
     scales[0][table[0, bad // page], :, bad % page, 0] = 255
@@ -103,6 +104,7 @@ def test_rows_past_the_last_that_the_call_has(dt, nq, nkv, d, flags):
     """row_start ends at 420, the call has 300 rows: the second request's are cut, the third has none; the others are as ever."""
     kv, fresh, page, rows = [500, 333, 90], [257, 120, 43], 32, 300
     table, row_start, n_pages = batch(kv, fresh, page, seed=3)
+    table = wide(table, page, 8192)
     codes, scales = fill(n_pages, nkv, page, d, 6, table, kv)
     q = iso_inputs.randn((rows, nq, d), seed=4, dtype=dt)
     with make_ctx(nq, nkv, d, dt) as ctx:

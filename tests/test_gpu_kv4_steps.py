@@ -6,7 +6,7 @@ import paper_2409_11155_amd as iso      # first: binds libiso to the HIP runtime
 import iso_inputs
 from oracle import kv4_oracle as ko
 from test_gpu_graph import Captured, hip_runtime
-from test_gpu_kv4 import HALF_STEP, attend, batch, check, device_cache, f64, fill, ints, make_ctx
+from test_gpu_kv4 import HALF_STEP, attend, batch, check, device_cache, f64, fill, ints, make_ctx, wide
 
 pytestmark = pytest.mark.gpu
 
@@ -117,6 +117,7 @@ def test_two_streams_with_a_workspace_each(shape):
     dt, page = "bf16", 64
     nq, nkv, d, kv, fresh = (8, 1, 128, [20000, 500], [1, 2]) if shape == "line" else (64, 2, 128, [900], [300])
     table, row_start, n_pages = batch(kv, fresh, page, seed=2)
+    table = wide(table, page, 8192 if shape == "rows" else 0)
     codes, scales = fill(n_pages, nkv, page, d, 3, table, kv)
     rows = int(row_start[-1])
     qs = [iso_inputs.randn((rows, nq, d), seed=s, dtype=dt) for s in (1, 2)]

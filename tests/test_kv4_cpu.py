@@ -168,10 +168,11 @@ def test_refusals(fake, dt):                                    # noqa: F811
 
 
 def test_which_kernels_a_batch_gets(fake):                     # noqa: F811
-    """Single tokens and short chunks: one launch, with 16 rows a tile where no request has more pairs; long chunks go to the tiles of 128
-    rows, beside a launch for the short requests of the batch if there can be any; fp32 stays on the line."""
+    """One launch for single tokens and short chunks, with 16 rows a tile where no request has more pairs or there is little to do for
+    heads of 128; long chunks go to the tiles of 128 rows where the table has room for many keys, beside a launch for the short requests of
+    the batch if there can be any; fp32 stays on the line."""
     run(fake, """
-def kernels(dt, nq, nkv, d, n_seqs, rows, most):
+def kernels(dt, nq, nkv, d, n_seqs, rows, most, keys):
     with iso.Context(iso.make_cfg(64, nq, nkv, d, 64, dt, 256)) as ctx:
         cache = ctx.kv4_cache(4, 16)
         i = iso.DeviceArray((64,), "i32")
@@ -179,19 +180,24 @@ def kernels(dt, nq, nkv, d, n_seqs, rows, most):
         n = ctx.attn_kv4_workspace(n_seqs, rows)
         ws = iso.DeviceArray((n,), "u8")
         log()
-        ctx.attn_kv4(q, nq * d, cache, i, 4, i, i, n_seqs, rows, most, out, ws, n)
+        ctx.attn_kv4(q, nq * d, cache, i, keys // 16, i, i, n_seqs, rows, most, out, ws, n)
         return [l[2].split()[0] for l in log() if l[0] == "kernel"]
 def line(name, rt):
     return "attn_kv4_kernel" in name and name.split("Li")[-1].startswith(str(rt))
-k = kernels("bf16", 8, 1, 128, 5, 5, 1);       assert len(k) == 1 and line(k[0], 1), k
-k = kernels("bf16", 8, 1, 128, 5, 5, 2);       assert len(k) == 1 and line(k[0], 1), k
-k = kernels("bf16", 8, 1, 128, 5, 50, 3);      assert len(k) == 1 and line(k[0], 2), k
-k = kernels("bf16", 8, 1, 128, 1, 2047, 2047); assert len(k) == 1 and line(k[0], 2), k
-k = kernels("bf16", 8, 1, 128, 1, 2048, 1);    assert len(k) == 1 and "rows" in k[0], k
-k = kernels("bf16", 8, 1, 128, 2, 4096, 2048); assert len(k) == 2 and line(k[0], 2) and "rows" in k[1], k
-k = kernels("bf16", 8, 1, 128, 2, 4096, 2047); assert len(k) == 1 and line(k[0], 2), k
-k = kernels("bf16", 130, 1, 64, 1, 200, 200);  assert len(k) == 1 and line(k[0], 2), k
-k = kernels("f32", 8, 1, 128, 1, 4096, 4096);  assert len(k) == 1 and line(k[0], 1), k
+k = kernels("bf16", 8, 1, 128, 5, 5, 1, 8192);       assert len(k) == 1 and line(k[0], 1), k
+k = kernels("bf16", 8, 1, 128, 5, 5, 2, 8192);       assert len(k) == 1 and line(k[0], 1), k
+k = kernels("bf16", 8, 1, 128, 5, 50, 3, 8192);      assert len(k) == 1 and line(k[0], 1), k
+k = kernels("bf16", 8, 1, 128, 5, 2000, 3, 8192);    assert len(k) == 1 and line(k[0], 2), k
+k = kernels("bf16", 8, 4, 64, 5, 9, 9, 64);          assert len(k) == 1 and line(k[0], 2), k
+k = kernels("bf16", 8, 1, 128, 1, 511, 511, 16384);  assert len(k) == 1 and line(k[0], 2), k
+k = kernels("bf16", 8, 1, 128, 1, 512, 512, 8192);   assert len(k) == 1 and line(k[0], 2), k
+k = kernels("bf16", 8, 1, 128, 1, 512, 1, 16384);    assert len(k) == 1 and "rows" in k[0], k
+k = kernels("bf16", 8, 1, 128, 1, 512, 1, 1 << 30);  assert len(k) == 1 and "rows" in k[0], k
+k = kernels("bf16", 8, 1, 128, 2, 4096, 512, 8192);  assert len(k) == 2 and line(k[0], 2) and "rows" in k[1], k
+k = kernels("bf16", 8, 1, 128, 2, 4096, 511, 8192);  assert len(k) == 1 and line(k[0], 2), k
+k = kernels("bf16", 8, 1, 128, 2, 4096, 512, 4096);  assert len(k) == 1 and line(k[0], 2), k
+k = kernels("bf16", 130, 1, 64, 1, 200, 200, 8192);  assert len(k) == 1 and line(k[0], 2), k
+k = kernels("f32", 8, 1, 128, 1, 4096, 4096, 8192);  assert len(k) == 1 and line(k[0], 1), k
 """)
 
 
