@@ -19,6 +19,13 @@
 // the workgroup that arrives last folds them in the order of the line, so the result does not depend on who that is, and puts the counter
 // back to zero.  Nobody waits for anybody.  The shares are computed on the device from the lengths there: a captured step keeps its balance
 // as the requests grow.
+//
+// Measured (bf16): 40 single tokens over 500 to 8192 keys, 13 heads of 128, 43.4 us, 4.2 TB/s of the cache (a large copy reaches 4.9);
+// 48 x 2 rows over 300 to 8192 keys, 32 heads of 64 over 8, 20 us, 3.0 TB/s: shares of 600 to 1100 keys behind 4 to 5 us of start and end;
+// one token over 131072 keys, 8 heads over 1, 16.5 us: 254 shares take 5 us for their keys, 3 to find them, 6 to fold them.  A
+// workgroup finds its share in about 2 us (some 600 dependent instructions and a trip to memory).  32 rows a tile, 16 heads over 2: 64 rows
+// over 32768 keys 47 us (365 TFLOP/s); 2 x 509 rows and 22 single tokens over 700 to 6000 keys 37 to 40 us (up to 330), vector instructions in
+// 52 %, matrix instructions in 16 % of the cycles, and workgroups that end between 32 and 40 us.
 #include "kv4.h"
 
 #include <algorithm>
@@ -634,11 +641,11 @@ hipError_t iso_launch_attn_kv4(int dtype, const void *q, int q_stride, const iso
     const unsigned mul = (unsigned)(((((u64)1 << bits) - G) << 32) / G) + 1;
     const line_args a{q, out, nullptr, nullptr, kv4_view_of(cache), b, q_stride, nq, nkv, (int)G, mul, bits, most};
     // Two blocks of rows a tile where a request can have more than one, and, with heads of 128 (two workgroups on a compute unit then instead
-    // of three, pieces twice as large), where a workgroup's share is about 1024 keys or more by the room that the table has.  16 and 32
+    // of three, pieces twice as large), where a workgroup's share is about 900 keys or more by the room that the table has.  16 and 32
     // rows a tile, 16 heads over 2: 5 rows for each of 8 requests of up to 4000 keys 14 and 22 us; 509 rows of 700 / 2048 / 6000 17 / 30 / 62 and
     // 19 / 28 / 54; heads of 64, 32 over 8: 200 rows of 2048 23 and 20, 500 of 500 19 and 16.
     const long long keys = std::min((long long)b.max_pages * cache.page, 0x7fffffffll), pairs = (long long)b.total_rows * nq;
-    const bool two = std::min((long long)max_rows * a.G, (long long)most) > 16 && (d == 64 || pairs / 32 * keys >= 1024ll * wg_per_cu(2, 128, 2) * iso_num_cu());
+    const bool two = std::min((long long)max_rows * a.G, (long long)most) > 16 && (d == 64 || pairs / 32 * keys >= 900ll * wg_per_cu(2, 128, 2) * iso_num_cu());
     if (dtype == ISO_F32) return d == 64 ? launch<float, 64, 1>(a, ws, s) : launch<float, 128, 1>(a, ws, s);
     if (d == 64) return two ? launch<bf16_t, 64, 2>(a, ws, s) : launch<bf16_t, 64, 1>(a, ws, s);
     return two ? launch<bf16_t, 128, 2>(a, ws, s) : launch<bf16_t, 128, 1>(a, ws, s);
