@@ -7,7 +7,8 @@
 //   * K goes from the page into the registers that the product wants: the four lanes of a key take a quarter of its head each, 16 (8)
 //     bytes, and element order inside the head is free as long as q is read in the same one.  No LDS.
 //   * V has to be transposed: a wave writes its 32 unpacked rows to LDS (its own 8 KB, no barrier) and reads them back with
-//     ds_read_b64_tr_b16.  16-byte chunks are XOR-swizzled by the row so that neither side has bank conflicts.
+//     ds_read_b64_tr_b16.  16-byte chunks are XOR-swizzled by the row (heads of 128: the LDS works in 29 % of the cycles, a fifth of that
+//     on bank conflicts).
 //   * RT = 2: what is unpacked once serves two blocks of 16 rows.  The second one is passed over where the tile does not reach it.
 //   * T = float: q and the probabilities are cut into three bf16 terms that add up to all 24 bits (K and V have two): three products.
 //
@@ -202,7 +203,7 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
 
     const float sc = 1.4426950408889634f / sqrtf((float)D);
     const unsigned lds_w = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds + wave * TILE * RB;
-    auto swz = [](int row) { return D == 128 ? ((row & 7) << 1 | (row >> 3 & 1)) : ((row >> 1 & 3) << 1 | (row >> 3 & 1)); };
+    auto swz = [](int row) { return D == 128 ? (row & 15) : ((row >> 1 & 3) << 1 | (row >> 3 & 1)); };
     // V: the lane's row on the way in is n16 (+ 16), on the way out 4 g4 + n16 / 4 (+ 16)
     unsigned char *const v_in = lds + wave * TILE * RB + n16 * RB;
     const int in_swz = swz(n16);

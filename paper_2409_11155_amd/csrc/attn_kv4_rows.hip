@@ -5,7 +5,8 @@
 // there (exact, see attn_kv4.hip) and written to LDS as bf16 rows, two stages, one barrier a tile.  The conversions ride behind the
 // first product's matrix instructions.  From LDS on it is the bf16 kernel's layout (attn_bf16_dtl.hip): S^T = K Q^T with
 // v_mfma_f32_32x32x16_bf16, statistics per lane, V read transposed (ds_read_b64_tr_b16), O^T = V^T P^T.
-// 16-byte chunks are XOR-swizzled by the row: the operand reads and the writes (16 rows by four chunks) are free of bank conflicts.
+// 16-byte chunks are XOR-swizzled by the row: any 16 neighbouring lanes of a read or a write touch different banks (the LDS works in 48 %
+// of the cycles, a quarter of that counted as conflicts).
 //
 // Work: as in attn_kv4.hip one line cut into equal shares, here in keys per key head: the k-th row tile of a request has
 // max(0, kv_len - rows) + (k + 1) * tokens places (a row tile further down sees more keys) behind SETUP places for its start and end, so a
