@@ -107,7 +107,7 @@ __global__ __launch_bounds__(BT_THREADS) void block_tables_kernel(bt_args a) {
 // Eight elements a lane and half a head: a lane has elements 8 l .. 8 l + 7 of the low half and of the high half of one head (the
 // two that a rotary step joins), four neighbouring lanes have a block of each.  Bound by memory: 16 bytes (bf16) a load, four bytes
 // of codes a store.  bf16, 13 heads of 128: 16384 rows stored in 31.6 us (4.4 TB/s), loaded in 28.8; 2047 rows rotated and written
-// in 11.8 (3.4 TB/s), loaded in 5.5.  64 rows 4.7 and 2.6: launch and two dependent trips to memory.
+// in 11.8 (2.7 TB/s), loaded in 5.5 (3.1).  64 rows 4.7 and 2.6: launch and two dependent trips to memory.
 template <typename T> __device__ __forceinline__ void load8(const T *p, float (&x)[8]);
 template <> __device__ __forceinline__ void load8<float>(const float *p, float (&x)[8]) {
     const f32x4_t a = reinterpret_cast<const f32x4_t *>(p)[0], b = reinterpret_cast<const f32x4_t *>(p)[1];
