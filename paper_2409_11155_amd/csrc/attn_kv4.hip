@@ -149,7 +149,7 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
     const int tid = threadIdx.x, lane = tid & 63, n16 = lane & 15, g4 = lane >> 4;
     const int wave = uniform(tid >> 6);
     const kv4_batch &b = a.b;
-    const int shift = a.c.page_shift, G = a.G, kvh = blockIdx.y;
+    const int shift = a.c.page_shift, G = a.G, kvh = blockIdx.x, wg = blockIdx.y;
     auto by_g = [&](int x) { return (int)((__umulhi((unsigned)x, a.g_mul) + (unsigned)x) >> a.g_bits); };
 
     // ---- the line: places in front of every request, and in all.  Every wave does this for itself, 64 requests at a time: no barrier,
@@ -177,13 +177,13 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
     // Any share does that covers the line (2^-17 more than its part, for the roundings); never less than MIN_SHARE keys, nor so little that
     // a tile has more pieces than can be folded.
     constexpr float MORE = 1.f + 0x1p-17f;
-    float share = fmaxf(fmaxf((float)all * (MORE * __builtin_amdgcn_rcpf((float)gridDim.x)), longest * (MORE / SPLITS)), (float)(G * MIN_SHARE));
+    float share = fmaxf(fmaxf((float)all * (MORE * __builtin_amdgcn_rcpf((float)gridDim.y)), longest * (MORE / SPLITS)), (float)(G * MIN_SHARE));
     // one round of folding instead of two where that lengthens a share by less than ROUND keys
     const float one_round = longest * (MORE / (GROUP - 1));
     if (one_round > share && one_round - share < (float)(G * ROUND)) share = one_round;
     u64 per = (u64)share + 1;
     per = uniform(per);
-    u64 at = (u64)blockIdx.x * per;
+    u64 at = (u64)wg * per;
     const u64 end = min(all, at + per);
     if (at >= end) return;
     const float inv_per = __builtin_amdgcn_rcpf((float)per);
@@ -241,7 +241,7 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
         const int ka = at == s0 ? 0 : key_at(at), kb = stop == s1 ? lim_hi : min(lim_hi, key_at(stop));
         auto owner = [&](int u) { return quotient(min(s1, s_keys + (u64)G * UNIT * (unsigned)(u + 1)) - 1, per, inv_per); };
         const int w0 = lim_hi > 0 ? owner(0) : quotient(s0, per, inv_per), w1 = lim_hi > UNIT ? owner((lim_hi - 1) / UNIT) : w0;
-        if ((int)blockIdx.x >= w0 && (int)blockIdx.x <= w1) {
+        if (wg >= w0 && wg <= w1) {
             // ---- this tile's rows
             bool real[RT];
             int lim[RT];
@@ -497,7 +497,7 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
                 // compute unit gets about 45 GB/s of pieces from memory: 126 of 4 KB took one workgroup 13 us.  16 rows, 16 heads over 2,
                 // 8192 keys, pieces of 16 KB: 25.7 us with groups of 16, 22.4 with smaller ones.)
                 constexpr int SLOT = slot_floats(D, RT) * 4;
-                const __amdgpu_buffer_rsrc_t rp = __builtin_amdgcn_make_buffer_rsrc((char *)a.part + (size_t)kvh * gridDim.x * 2 * SLOT, 0, (int)(gridDim.x * 2 * SLOT), 0x00020000);
+                const __amdgpu_buffer_rsrc_t rp = __builtin_amdgcn_make_buffer_rsrc((char *)a.part + (size_t)kvh * gridDim.y * 2 * SLOT, 0, (int)(gridDim.y * 2 * SLOT), 0x00020000);
                 auto index = [&](int w) { return 2 * w + (w == w0 ? 1 : 0); };      // a workgroup's tile from before, or the one begun here
                 auto park = [&](int w) {
                     const unsigned p = (unsigned)index(w) * SLOT;
@@ -569,16 +569,16 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
                         }
                     }
                 };
-                unsigned *const cnt = a.cnt + (size_t)kvh * gridDim.x * 3;     // two of pieces and one of groups a workgroup
+                unsigned *const cnt = a.cnt + (size_t)kvh * gridDim.y * 3;     // two of pieces and one of groups a workgroup
                 const int n = w1 - w0 + 1, bits = n <= GROUP || n > GROUP * GROUP / 4 ? 4 : 3, size = 1 << bits;
-                const int group = ((int)blockIdx.x - w0) >> bits, head = w0 + (group << bits), groups = (n + size - 1) >> bits, members = min(size, n - (group << bits));
-                park(blockIdx.x);
+                const int group = (wg - w0) >> bits, head = w0 + (group << bits), groups = (n + size - 1) >> bits, members = min(size, n - (group << bits));
+                park(wg);
                 writes = last_of(cnt + index(head), members);
                 if (writes) {
                     fold(head, 1, members);
                     if (groups > 1) {
                         park(head);                      // in the place of the group's first piece, which is read
-                        writes = last_of(cnt + 2 * gridDim.x + w0, groups);
+                        writes = last_of(cnt + 2 * gridDim.y + w0, groups);
                         if (writes) fold(w0, size, groups);
                     }
                 }
@@ -620,7 +620,10 @@ template <typename T, int D, int RT> hipError_t launch(line_args a, void *ws, hi
     const int wgs = line_wgs(wg_per_cu(sizeof(T), D, RT), a.nkv, iso_num_cu());
     a.cnt = (unsigned *)ws;
     a.part = (float *)((char *)ws + counters(a.nkv, iso_num_cu()));
-    hipLaunchKernelGGL((attn_kv4_kernel<T, D, RT>), dim3(wgs, a.nkv), dim3(THREADS), 0, s, a);
+    // The key heads run fastest: shares of the same number are alike in all heads, and where they are fewer than the workgroups, the ones
+    // that have some are the first.  (Shares fastest: one compute unit got the same shares of several heads; 32 heads of 64 over 8, 2 rows
+    // over 1616 keys 11.3 us, now 8.0, 7 x 4 rows over up to 2000 12.8 and 10.0.)
+    hipLaunchKernelGGL((attn_kv4_kernel<T, D, RT>), dim3(a.nkv, wgs), dim3(THREADS), 0, s, a);
     return hipGetLastError();
 }
 

@@ -82,7 +82,7 @@ template <int D> __global__ __launch_bounds__(THREADS, 2) void attn_kv4_rows_ker
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = uniform(tid >> 6);
     const kv4_batch &b = a.b;
-    const int shift = a.c.page_shift, G = a.G, kvh = blockIdx.y;
+    const int shift = a.c.page_shift, G = a.G, kvh = blockIdx.x, wg = blockIdx.y;
     const uint32_t lds_addr = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds;
     const int lcol = lane & 31, lgrp = lane >> 5;
 
@@ -115,8 +115,8 @@ template <int D> __global__ __launch_bounds__(THREADS, 2) void attn_kv4_rows_ker
     };
     u64 incl = scan(mine);
     const u64 all = uniform((u64)__shfl(incl, 63, 64));
-    const u64 per = uniform(max(max((all + gridDim.x - 1) / gridDim.x, (u64)MIN_SHARE), (longest + PIECES - 1) / PIECES));
-    u64 at = (u64)blockIdx.x * per;
+    const u64 per = uniform(max(max((all + gridDim.y - 1) / gridDim.y, (u64)MIN_SHARE), (longest + PIECES - 1) / PIECES));
+    u64 at = (u64)wg * per;
     const u64 end = min(all, at + per);
     if (at >= end) return;
     const double inv_per = 1.0 / (double)per;
@@ -177,7 +177,7 @@ template <int D> __global__ __launch_bounds__(THREADS, 2) void attn_kv4_rows_ker
         const int ka = key_at(at), kb = stop == s0 + span ? lim_hi : min(lim_hi, key_at(stop));
         auto owner = [&](int block) { return share_of(min(s0 + span, s0 + SETUP + (u64)BN * (block + 1)) - 1); };
         const int w_a = lim_hi > 0 ? owner(0) : share_of(s0), w_b = lim_hi > 0 ? owner((lim_hi - 1) / BN) : w_a;
-        const bool has_part = (int)blockIdx.x >= w_a && (int)blockIdx.x <= w_b;
+        const bool has_part = wg >= w_a && wg <= w_b;
         if (has_part) {
             const int row = wave * 32 + lcol, t = row / G, head = kvh * G + (row - t * G);
             const bool real = t < toks;
@@ -400,10 +400,10 @@ template <int D> __global__ __launch_bounds__(THREADS, 2) void attn_kv4_rows_ker
             bool writes = true;
             if (w_b > w_a) {
                 const __amdgpu_buffer_rsrc_t rp = __builtin_amdgcn_make_buffer_rsrc(
-                    (void *)(a.part + (size_t)kvh * gridDim.x * 2 * part_bytes<D>()), 0, (int)(gridDim.x * 2 * part_bytes<D>()), 0x00020000);
+                    (void *)(a.part + (size_t)kvh * gridDim.y * 2 * part_bytes<D>()), 0, (int)(gridDim.y * 2 * part_bytes<D>()), 0x00020000);
                 auto slot = [&](int w) { return (unsigned)(2 * w + (w == w_a ? 1 : 0)) * part_bytes<D>(); };
                 {
-                    const unsigned p = slot(blockIdx.x);
+                    const unsigned p = slot(wg);
 #pragma unroll
                     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -417,7 +417,7 @@ template <int D> __global__ __launch_bounds__(THREADS, 2) void attn_kv4_rows_ker
                 __builtin_amdgcn_s_waitcnt(0);       // my stores have reached memory ...
                 __syncthreads();                     // ... and so have everybody's, before the arrival is counted
                 if (tid == 0) {
-                    unsigned *cnt = a.cnt + kvh * gridDim.x + w_a;
+                    unsigned *cnt = a.cnt + kvh * gridDim.y + w_a;
                     const unsigned n = __hip_atomic_fetch_add(cnt, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
                     last_arriver = n == (unsigned)(w_b - w_a);
                     if (last_arriver) __hip_atomic_store(cnt, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
@@ -496,7 +496,7 @@ hipError_t iso_launch_attn_kv4_rows(const void *q, int q_stride, const iso_kv4 &
     static iso_dev_mask allowed[2];
     const void *kernel = d == 64 ? (const void *)attn_kv4_rows_kernel<64> : (const void *)attn_kv4_rows_kernel<128>;
     if (hipError_t e = iso_allow_lds(kernel, lds, &allowed[d == 64]); e != hipSuccess) return e;
-    if (d == 64) hipLaunchKernelGGL(attn_kv4_rows_kernel<64>, dim3(wgs, nkv), dim3(THREADS), lds, s, a);
-    else hipLaunchKernelGGL(attn_kv4_rows_kernel<128>, dim3(wgs, nkv), dim3(THREADS), lds, s, a);
+    if (d == 64) hipLaunchKernelGGL(attn_kv4_rows_kernel<64>, dim3(nkv, wgs), dim3(THREADS), lds, s, a);
+    else hipLaunchKernelGGL(attn_kv4_rows_kernel<128>, dim3(nkv, wgs), dim3(THREADS), lds, s, a);
     return hipGetLastError();
 }
