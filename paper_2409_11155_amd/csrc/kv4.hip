@@ -106,8 +106,8 @@ __global__ __launch_bounds__(BT_THREADS) void block_tables_kernel(bt_args a) {
 // ---- rows into pages, and back -----------------------------------------------------------------
 // Eight elements a lane and half a head: a lane has elements 8 l .. 8 l + 7 of the low half and of the high half of one head (the
 // two that a rotary step joins), four neighbouring lanes have a block of each.  Bound by memory: 16 bytes (bf16) a load, four bytes
-// of codes a store.  bf16, 13 heads of 128: 16384 rows stored in 31.6 us (4.4 TB/s), loaded in 28.8; 2047 rows rotated and written
-// in 11.8 (2.7 TB/s), loaded in 5.5 (3.1).  64 rows 4.7 and 2.6: launch and two dependent trips to memory.
+// of codes a store.  bf16, 13 heads of 128: 16384 rows stored in 30 us (4.6 TB/s), loaded in 27; 2047 rows rotated and written
+// in 9.8 (3.3 TB/s), loaded in 5.8 (2.9).  64 rows 4.0 and 2.5: launch and two dependent trips to memory.
 template <typename T> __device__ __forceinline__ void load8(const T *p, float (&x)[8]);
 template <> __device__ __forceinline__ void load8<float>(const float *p, float (&x)[8]) {
     const f32x4_t a = reinterpret_cast<const f32x4_t *>(p)[0], b = reinterpret_cast<const f32x4_t *>(p)[1];
@@ -201,11 +201,13 @@ __global__ __launch_bounds__(256) void kv4_write_kernel(T *qkv, T *q_out, const 
     const unsigned th = blockIdx.x * (256u / LPH) + threadIdx.x / LPH;         // (row, head); fewer than 2^31 of them
     const int l = threadIdx.x % LPH;
     if (th >= (unsigned)n_rows * heads) return;        // a head's lanes leave together
-    const int t = (int)(th / heads), h = (int)(th - (unsigned)t * heads);
-    const int nqk = ROPE ? nq + nkv : nkv;             // heads in front of v
-    const bool is_q = ROPE && h < nq, is_v = h >= nqk;
-    const int g = is_q ? 0 : is_v ? h - nqk : ROPE ? h - nq : h;
-    const T *src = ROPE ? qkv + (size_t)th * D : (is_v ? v_rows : k_rows) + ((size_t)t * nkv + g) * D;
+    // All rows' k heads, then all q, then all v: a wave does one of them (key heads are rotated in 64 bits, and with heads in a row's order
+    // nearly every wave had one: 2047 rows of 13 heads each 12.6 us, now 9.8; 2048 of 16 heads over 2 7.7 and 6.0).
+    const unsigned k_all = (unsigned)n_rows * nkv, q_end = k_all + (ROPE ? (unsigned)n_rows * nq : 0);
+    const bool is_k = th < k_all, is_q = ROPE && !is_k && th < q_end, is_v = !is_k && !is_q;
+    const unsigned r = th - (is_k ? 0 : is_q ? k_all : q_end), per = is_q ? nq : nkv;
+    const int t = (int)(r / per), g = (int)(r - (unsigned)t * per);
+    const T *src = ROPE ? qkv + ((size_t)t * heads + (is_q ? 0 : is_v ? nq + nkv : nq) + g) * D : (is_v ? v_rows : k_rows) + (size_t)r * D;
     float lo[8], hi[8];
     load8<T>(src + 8 * l, lo);                         // on their way before it is known where they go
     load8<T>(src + D / 2 + 8 * l, hi);
@@ -225,7 +227,7 @@ __global__ __launch_bounds__(256) void kv4_write_kernel(T *qkv, T *q_out, const 
                 lo[i] = fmaf(a, cs[i], -(b * sn[i]));
                 hi[i] = fmaf(b, cs[i], a * sn[i]);
             }
-            T *dst = q_out ? q_out + ((size_t)t * nq + h) * D : const_cast<T *>(src);
+            T *dst = q_out ? q_out + (size_t)r * D : const_cast<T *>(src);
             store8(dst + 8 * l, lo);
             store8(dst + D / 2 + 8 * l, hi);
             return;
@@ -249,9 +251,10 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(kv4_view c, const int *__
     const unsigned th = blockIdx.x * (256u / LPH) + threadIdx.x / LPH;         // (row, head); fewer than 2^31 of them
     const int l = threadIdx.x % LPH;
     if (th >= (unsigned)n_rows * 2u * nkv) return;
-    const int t = (int)(th / (2u * nkv)), h = (int)(th - (unsigned)t * (2u * nkv));
-    const bool is_v = h >= nkv;
-    const int g = is_v ? h - nkv : h;
+    const unsigned k_all = (unsigned)n_rows * nkv;             // all rows' k heads, then all v
+    const bool is_v = th >= k_all;
+    const unsigned r = is_v ? th - k_all : th;
+    const int t = (int)(r / (unsigned)nkv), g = (int)(r - (unsigned)t * nkv);
     const int slot = slots[t];
     if (slot < 0 || (slot >> c.page_shift) >= c.n_pages) return;
     const size_t tok = token_at<D>(c, nkv, slot, g);
@@ -260,7 +263,7 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(kv4_view c, const int *__
     const bf16x2_t p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, f, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, f, 1);
     const bf16x2_t p2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, f, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, f, 3);
     const float x[8] = {(float)p0[0], (float)p0[1], (float)p1[0], (float)p1[1], (float)p2[0], (float)p2[1], (float)p3[0], (float)p3[1]};
-    store8((is_v ? v_rows : k_rows) + ((size_t)t * nkv + g) * D + 8 * l, x);
+    store8((is_v ? v_rows : k_rows) + (size_t)r * D + 8 * l, x);
 }
 
 template <typename T, int D>
