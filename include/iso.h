@@ -323,7 +323,7 @@ int iso_gemm_fp8(iso_ctx *ctx, const void *a8, const float *sa, const void *w8, 
  *   (Bytes 0, 1, 253 and 254 are not written, and what they stand for is not defined.)
  *   Layout.  k, v [n_pages, nkv, page, d/2] bytes; k_scale, v_scale [n_pages, nkv, page, d/32] bytes.  A token's slot is its page's
  *   number * page + its place in the page.  Both context types (ISO_F32, ISO_BF16) read and write it; nothing in it depends on the
- *   type.  The library never looks at a page that no table or slot names.
+ *   type.  What a page holds that no table or slot names has no effect (page 0 may be read in place of one that is not there).
  * Pointers are 16-byte aligned, int pointers 4-byte (else ISO_ERR_SHAPE).  These calls use nothing of the context but its
  * configuration and rotary table, run on any stream of the context's device (which has to be current, else ISO_ERR_HIP), and may
  * be recorded into a HIP graph and replayed. */
