@@ -377,7 +377,8 @@ int iso_kv4_load(iso_ctx *ctx, const iso_kv4 *cache, const int *slots, void *k, 
  *   context, of any shape that fits).  Calls that may overlap in time, replays of a graph among them, need one each.
  *   q, out and ws must not overlap (ISO_ERR_SHAPE).
  * Results do not depend on the order in which workgroups run.
- * Errors: NULL, n_seqs outside [1, 4096], total_rows, max_rows or max_pages < 1, q_stride (ISO_ERR_SHAPE), ws too small
+ * Errors: NULL, n_seqs outside [1, 4096], total_rows, max_rows or max_pages < 1, max_pages * page above 2^31 - 1024, q_stride
+ * (ISO_ERR_SHAPE), ws too small
  * (ISO_ERR_WORKSPACE). */
 int iso_attn_kv4_workspace(iso_ctx *ctx, int n_seqs, int total_rows, size_t *bytes);
 int iso_attn_kv4(iso_ctx *ctx, const void *q, int q_stride, const iso_kv4 *cache, const int *block_table, int max_pages,

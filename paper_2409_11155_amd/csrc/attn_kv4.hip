@@ -237,7 +237,8 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
         const int lim_lo = uniform(limit(by_g(first_pair))), lim_hi = uniform(limit(by_g(min(pairs, first_pair + ROWS) - 1)));
         // ---- the piece's keys (the share begins and ends at multiples of UNIT keys of the tile), and the workgroups that have pieces
         const u64 s_keys = s0 + (u64)G * SETUP;
-        auto key_at = [&](u64 place) { return place < s_keys ? 0 : quotient(place - s_keys, (u64)G * UNIT, inv_unit) * UNIT; };
+        // (a tile's places may lie past its last key, and past 31 bits: the limit is beyond every key)
+        auto key_at = [&](u64 place) { return place < s_keys ? 0 : min(quotient(place - s_keys, (u64)G * UNIT, inv_unit), KV4_MAX_KEYS / UNIT) * UNIT; };
         const int ka = at == s0 ? 0 : key_at(at), kb = stop == s1 ? lim_hi : min(lim_hi, key_at(stop));
         auto owner = [&](int u) { return quotient(min(s1, s_keys + (u64)G * UNIT * (unsigned)(u + 1)) - 1, per, inv_per); };
         const int w0 = lim_hi > 0 ? owner(0) : quotient(s0, per, inv_per), w1 = lim_hi > UNIT ? owner((lim_hi - 1) / UNIT) : w0;
@@ -648,7 +649,7 @@ hipError_t iso_launch_attn_kv4(int dtype, const void *q, int q_stride, const iso
     // of three, pieces twice as large), where a workgroup's share is about 900 keys or more by the room that the table has.  16 and 32
     // rows a tile, 16 heads over 2: 5 rows for each of 8 requests of up to 4000 keys 14 and 22 us; 509 rows of 700 / 2048 / 6000 17 / 30 / 62 and
     // 19 / 28 / 54; heads of 64, 32 over 8: 200 rows of 2048 23 and 20, 500 of 500 19 and 16.
-    const long long keys = std::min((long long)b.max_pages * cache.page, 0x7fffffffll), pairs = (long long)b.total_rows * nq;
+    const long long keys = (long long)b.max_pages * cache.page, pairs = (long long)b.total_rows * nq;
     const bool two = std::min((long long)max_rows * a.G, (long long)most) > 16 && (d == 64 || pairs / 32 * keys >= 900ll * wg_per_cu(2, 128, 2) * iso_num_cu());
     if (dtype == ISO_F32) return d == 64 ? launch<float, 64, 1>(a, ws, s) : launch<float, 128, 1>(a, ws, s);
     if (d == 64) return two ? launch<bf16_t, 64, 2>(a, ws, s) : launch<bf16_t, 64, 1>(a, ws, s);

@@ -173,7 +173,7 @@ template <int D> __global__ __launch_bounds__(THREADS, 2) void attn_kv4_rows_ker
         auto limit = [&](int tok) { return (int)max(0ll, min((long long)rq.keys, (long long)rq.base + tok + 1)); };
         const int lim_lo = limit(tok0), lim_hi = limit(tok0 + toks - 1);
         // keys of this piece, and the workgroups that have pieces of the tile
-        auto key_at = [&](u64 place) { return place - s0 < SETUP ? 0 : (int)((place - s0 - SETUP) / BN) * BN; };
+        auto key_at = [&](u64 place) { return place - s0 < SETUP ? 0 : (int)min((place - s0 - SETUP) / BN, (u64)(KV4_MAX_KEYS / BN)) * BN; };      // (places may pass 31 bits)
         const int ka = key_at(at), kb = stop == s0 + span ? lim_hi : min(lim_hi, key_at(stop));
         auto owner = [&](int block) { return share_of(min(s0 + span, s0 + SETUP + (u64)BN * (block + 1)) - 1); };
         const int w_a = lim_hi > 0 ? owner(0) : share_of(s0), w_b = lim_hi > 0 ? owner((lim_hi - 1) / BN) : w_a;

@@ -913,7 +913,7 @@ Kv4Launch kv4_launch(const iso_cfg &c, int n_seqs, int total_rows, int max_rows,
     const int ncu = iso_num_cu();
     const bool can = c.dtype == ISO_BF16 && c.n_q_heads / c.n_kv_heads <= 64;
     auto many = [&](int rows) { return can && (long long)rows * c.n_q_heads >= 4096; };
-    const long long work = (long long)total_rows * c.n_q_heads * std::min(keys, 0x7fffffffll);
+    const long long work = (long long)total_rows * c.n_q_heads * keys;
     Kv4Launch l;
     l.rows = n_seqs == 1 ? many(total_rows) && work > 1ll << 25 : many(std::min(max_rows, total_rows)) && work > 1ll << 27;
     l.line = !l.rows || n_seqs > 1;
@@ -1500,6 +1500,8 @@ int iso_attn_kv4(iso_ctx *ctx, const void *q, int q_stride, const iso_kv4 *cache
     ISO_TRY(check_kv4(cache));
     const iso_cfg &c = ctx->cfg;
     if (max_rows < 1 || max_pages < 1) return fail(ISO_ERR_SHAPE, "max_rows=%d and max_pages=%d must be positive", max_rows, max_pages);
+    if ((long long)max_pages * cache->page > KV4_MAX_KEYS)
+        return fail(ISO_ERR_SHAPE, "max_pages=%d of %d tokens: at most %d tokens of a request", max_pages, cache->page, KV4_MAX_KEYS);
     if (q_stride < c.n_q_heads * c.head_dim || q_stride % 8)
         return fail(ISO_ERR_SHAPE, "q_stride=%d must be a multiple of 8, at least %d", q_stride, c.n_q_heads * c.head_dim);
     size_t need = 0;

@@ -6,6 +6,7 @@
 
 constexpr int KV4_BLOCK = 32;
 constexpr int KV4_MAX_SEQS = 4096;      // requests in one call: their prefix sums are kept in LDS
+constexpr int KV4_MAX_KEYS = 0x7fffffff - 1023;      // tokens that a request's table has room for: key counters run up to 300 past the last one
 
 // Device view of an iso_kv4.  Strides in bytes; a page holds every kv head's tokens, a head's tokens are contiguous.
 struct kv4_view {
