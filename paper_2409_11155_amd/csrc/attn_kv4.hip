@@ -66,10 +66,11 @@ __device__ __forceinline__ bf16x4_v read_tr(unsigned addr) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4_v *)(uintptr_t)addr);
 }
 
-// x as a sum of NP bf16 terms: rounded to nearest (NP = 1), or cut off so that three terms are all of x.
+// x as a sum of NP bf16 terms: the nearest, and the nearest of what is left (NP = 1, 2), or cut off so that three terms are all of x.
 template <int NP> __device__ __forceinline__ void split(float x, bf16_t (&t)[NP]) {
-    if constexpr (NP == 1) {
+    if constexpr (NP < 3) {
         t[0] = (bf16_t)x;
+        if constexpr (NP == 2) t[1] = (bf16_t)(x - (float)t[0]);
     } else {
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
@@ -137,11 +138,12 @@ __device__ __forceinline__ u64 lane_of(u64 x, int lane) {
 
 template <typename T, int D, int RT>
 __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4_kernel(line_args a) {
-    constexpr int NP = sizeof(T) == 4 ? 3 : 1;
+    constexpr int NP = sizeof(T) == 4 ? 3 : 1;               // bf16 terms of a query element ...
+    constexpr int NV = sizeof(T) == 4 ? 3 : kv4_terms(D);    // ... and of a probability
     constexpr int ROWS = 16 * RT;
     constexpr int WPL = D / 32;              // code words (8 elements) a lane takes of a key
     constexpr int RB = 2 * D;                // bytes of an unpacked row
-    constexpr int VG = D == 64 ? 2 : 1;      // blocks of 16 dims of V that are read at a time
+    constexpr int VG = D == 64 && RT == 1 ? 2 : 1;      // blocks of 16 dims of V that are read at a time (two would not fit the registers beside two row blocks)
     __shared__ __attribute__((aligned(1024))) unsigned char lds[WAVES * TILE * RB];
     __shared__ float ml[2][WAVES][16];
     __shared__ int last_arriver;
@@ -394,7 +396,7 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
                         for (int dt = 0; dt < D / 16; ++dt) o[x][dt] *= alpha;
                     }
                 }
-                bf16x8_t pb[RT][NP];
+                bf16x8_t pb[RT][NV];
 #pragma unroll
                 for (int x = 0; x < N; ++x) {
                     const float neg_m = m_run[x] == -INFINITY ? 0.f : -m_run[x];
@@ -404,10 +406,10 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
                         for (int e = 0; e < 4; ++e) {
                             const float p = __builtin_amdgcn_exp2f(fmaf(s[x][h][e], sc, neg_m));
                             l_run[x] += p;
-                            bf16_t part[NP];           // bf16: half a step of 2^-8 for the product, the sum keeps 24 bits
-                            split<NP>(p, part);
+                            bf16_t part[NV];
+                            split<NV>(p, part);
 #pragma unroll
-                            for (int y = 0; y < NP; ++y) pb[x][y][4 * h + e] = part[y];
+                            for (int y = 0; y < NV; ++y) pb[x][y][4 * h + e] = part[y];
                         }
                 }
 #pragma unroll
@@ -417,7 +419,7 @@ __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4
 #pragma unroll
                     for (int i = 0; i < VG; ++i)
 #pragma unroll
-                        for (int p = 0; p < NP; ++p)
+                        for (int p = 0; p < NV; ++p)
 #pragma unroll
                             for (int x = 0; x < N; ++x)
                                 o[x][VG * grp + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[grp & 1][i], pb[x][p], o[x][VG * grp + i], 0, 0, 0);

@@ -73,6 +73,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t beyond(unsigned char *p, u64 a
 template <int D> __global__ __launch_bounds__(THREADS, 2) void attn_kv4_rows_kernel(rows_args a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int WPL = D / 32;                  // code words (8 elements) a lane takes of a key: a quarter of its head
+    constexpr int NV = kv4_terms(D);             // bf16 terms of a probability
     constexpr int ROW_B = 2 * D, TILE_B = BN * ROW_B, STAGE_B = 2 * TILE_B;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     __shared__ u64 nan_v[2][4];                  // per stage and loading wave: V blocks that are NaN (masked tiles only)
@@ -273,7 +274,7 @@ template <int D> __global__ __launch_bounds__(THREADS, 2) void attn_kv4_rows_ker
                     __builtin_amdgcn_sched_barrier(0);
                 }
             };
-            auto softmax = [&](int k0, int stage, bool mask, f32x16_t (&s)[2], bf16x8_t (&pb)[2][2]) {
+            auto softmax = [&](int k0, int stage, bool mask, f32x16_t (&s)[2], bf16x8_t (&pb)[NV][2][2]) {
                 if (mask) {
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
@@ -309,12 +310,13 @@ template <int D> __global__ __launch_bounds__(THREADS, 2) void attn_kv4_rows_ker
                     for (int r = 0; r < 16; ++r) {
                         const float p = __builtin_amdgcn_exp2f(fmaf(s[sub][r], sc, neg_m));
                         psum += p;
-                        pb[sub][r / 8][r % 8] = (bf16_t)p;                     // a bf16 probability: half a step of 2^-8, the sum keeps 24 bits
+                        pb[0][sub][r / 8][r % 8] = (bf16_t)p;
+                        if constexpr (NV == 2) pb[1][sub][r / 8][r % 8] = (bf16_t)(p - (float)(bf16_t)p);
                     }
                 l_run += psum;
             };
             // O^T += V^T P^T: k-slots 8 lgrp .. +8 of step (sub, t) hold keys 32 sub + 16 t + 4 lgrp + {0..3} and the same + 8
-            auto second = [&](int stage, bf16x8_t (&pb)[2][2]) {
+            auto second = [&](int stage, bf16x8_t (&pb)[NV][2][2]) {
                 bf16x8_t vf[2][4];
                 const uint32_t base = lds_addr + (uint32_t)(stage * STAGE_B + TILE_B + v_row * ROW_B + v_byte);
                 auto read_v = [&](int buf, int dt) {
@@ -337,7 +339,9 @@ template <int D> __global__ __launch_bounds__(THREADS, 2) void attn_kv4_rows_ker
                     }
 #pragma unroll
                     for (int st = 0; st < 4; ++st)
-                        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[dt & 1][st], pb[st >> 1][st & 1], o[dt], 0, 0, 0);
+#pragma unroll
+                        for (int p = 0; p < NV; ++p)
+                            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[dt & 1][st], pb[p][st >> 1][st & 1], o[dt], 0, 0, 0);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             };
@@ -374,7 +378,7 @@ template <int D> __global__ __launch_bounds__(THREADS, 2) void attn_kv4_rows_ker
                     const bool mask = masked(k0);
                     if (masked(k0 + BN)) guard(k0 + BN, stage ^ 1, next);
                     f32x16_t s[2];
-                    bf16x8_t pb[2][2];
+                    bf16x8_t pb[NV][2][2];
                     // Products go before the other workgroup's softmax: 2048 rows over 32768 keys 352 -> 330 us, over 131072 1197 -> 1131.
                     __builtin_amdgcn_s_setprio(1);
                     scores(stage, s, [&](int grp, int of) {                    // a word of K and one of V behind each group
