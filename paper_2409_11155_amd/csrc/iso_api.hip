@@ -877,10 +877,11 @@ int check_device(const iso_ctx *ctx) {
     return ISO_OK;
 }
 
-// Rows of a write or a read: (row, head) pairs are counted in 31 bits.
+// Rows of a write or a read: a lane takes 8 or 16 elements, and a launch has fewer than 2^32 lanes (and so fewer than 2^31 (row, head) pairs).
 int check_rows(const iso_cfg &c, int T) {
     if (T < 1) return fail(ISO_ERR_SHAPE, "T=%d must be positive", T);
-    if ((long long)T * (c.n_q_heads + 2 * c.n_kv_heads) >= (1ll << 31)) return fail(ISO_ERR_SHAPE, "T=%d rows of %d heads: fewer than 2^31 together", T, c.n_q_heads + 2 * c.n_kv_heads);
+    const long long heads = (long long)c.n_q_heads + 2ll * c.n_kv_heads;
+    if (T * heads >= (1ll << 35) / c.head_dim) return fail(ISO_ERR_SHAPE, "T=%d rows of %lld heads of %d: fewer than 2^35 elements together", T, heads, c.head_dim);
     return ISO_OK;
 }
 
@@ -1516,6 +1517,8 @@ int iso_attn_kv4(iso_ctx *ctx, const void *q, int q_stride, const iso_kv4 *cache
     const kv4_batch b{block_table, row_start, kv_len, max_pages, n_seqs, total_rows};
     const hipStream_t s = (hipStream_t)stream;
     if (ctx->flags & ISO_FLAG_SIMPLE_ATTN) {
+        if (total_rows > (1 << 26) - 4 || c.n_q_heads > 65535)       // four rows a workgroup of 256 lanes, a grid row a head
+            return fail(ISO_ERR_SHAPE, "total_rows=%d of %d heads: ISO_FLAG_SIMPLE_ATTN takes fewer than 2^26 - 3 rows and 2^16 heads", total_rows, c.n_q_heads);
         LAUNCH_TRY(ISO_K_ATTN, s, iso_launch_attn_kv4_simple(c.dtype, q, q_stride, *cache, b, out, c.n_q_heads, c.n_kv_heads, c.head_dim, s),
                    "kv4 attention");
         return ISO_OK;

@@ -26,3 +26,36 @@ for dt, flags in (("bf16", 0), ("bf16", iso.ISO_FLAG_SIMPLE_ATTN), ("f32", 0)):
                         assert not ok and e.code == -2 and "at most 2147482624 tokens" in str(e), (page, rows, pages, e)
                         assert log() == []
 """)
+
+
+def test_more_rows_than_a_launch_has_lanes_for(fake):          # noqa: F811
+    """Every launch that is let through has fewer than 2^32 lanes.  (No memory is touched: the addresses are far apart and nowhere.)"""
+    run(fake, """
+L = iso.load()
+def lanes():
+    return [l for l in log() if l[0] == "kernel"]
+far = [(i + 1) << 44 for i in range(8)]
+for dt, nq, nkv, d in (("bf16", 1, 1, 128), ("bf16", 8, 1, 128), ("bf16", 13, 13, 64), ("f32", 4, 4, 64), ("bf16", 1, 1, 64)):
+    with iso.Context(iso.make_cfg(64, nq, nkv, d, 64, dt, 256)) as ctx:
+        c = ctypes.byref(iso.IsoKv4(far[0], far[1], far[2], far[3], 4, 16))
+        def calls(T):
+            return [L.iso_rope_kv4_write(ctx._h, far[4], None, c, far[6], far[7], T, None), L.iso_rope_kv4_write(ctx._h, far[4], far[5], c, far[6], far[7], T, None),
+                    L.iso_kv4_store(ctx._h, far[4], far[5], c, far[6], T, None), L.iso_kv4_load(ctx._h, c, far[6], far[4], far[5], T, None)]
+        log()
+        most = (2 ** 35 // d - 1) // (nq + 2 * nkv)
+        assert calls(min(most, 2 ** 31 - 1)) == [0] * 4, iso.last_error()
+        assert len(lanes()) == 4
+        for lanes_each in (16, 8):
+            assert most * (nq + 2 * nkv) * d // lanes_each <= 2 ** 32
+        for T in (most + 1, 2 * most, 2 ** 31 - 1):
+            if most < T < 2 ** 31:
+                assert calls(T) == [-2] * 4 and "2^35" in iso.last_error(), T
+        assert lanes() == []
+        ctx.set_flags(iso.ISO_FLAG_SIMPLE_ATTN)
+        n = ctypes.c_size_t()
+        for rows, want in ((2 ** 26 - 4, 0), (2 ** 26 - 3, -2)):
+            if rows * nq < 2 ** 31:
+                assert L.iso_attn_kv4_workspace(ctx._h, 1, rows, ctypes.byref(n)) == 0
+                assert L.iso_attn_kv4(ctx._h, far[4], nq * d, c, far[6], 4, far[6], far[6], 1, rows, rows, far[5], far[7], n, None) == want, iso.last_error()
+        log()
+""")
