@@ -356,13 +356,13 @@ int iso_block_tables(iso_ctx *ctx, const int *cached, const int *fresh, int n_se
  * to slots[t].  The rotated q goes to q_out [T, nq, d], or back into qkv where q_out is NULL.  k is rotated in 64 bits (from the same
  * fp32 table), so that its codes are those of the exact value.  A row whose position is outside [0, max_seq) is left alone, q too; one
  * whose slot is not in the cache has only its q rotated.  Slots must differ from one another (else that slot's content is undefined).
- * q_out must not overlap qkv (ISO_ERR_SHAPE).
+ * What is written (q_out, or qkv without it, and the cache's four buffers) must not overlap anything else of the call (ISO_ERR_SHAPE).
  * Errors: NULL, T < 1, T * (nq + 2 nkv) * d not below 2^35, a cache that is none (ISO_ERR_SHAPE). */
 int iso_rope_kv4_write(iso_ctx *ctx, void *qkv, void *q_out, const iso_kv4 *cache, const int *positions, const int *slots, int T,
                        void *stream);
 /* Rows k, v [T, nkv, d] of cfg.dtype, as a prefill leaves them in its cache, into slots (rows without one are passed over), and the
  * values that the slots hold back into rows (rows without one are left as they were).  What is loaded is exact in both types.
- * Errors: as iso_rope_kv4_write. */
+ * Errors: as iso_rope_kv4_write; what is written must not overlap anything else here either. */
 int iso_kv4_store(iso_ctx *ctx, const void *k, const void *v, const iso_kv4 *cache, const int *slots, int T, void *stream);
 int iso_kv4_load(iso_ctx *ctx, const iso_kv4 *cache, const int *slots, void *k, void *v, int T, void *stream);
 
@@ -376,7 +376,7 @@ int iso_kv4_load(iso_ctx *ctx, const iso_kv4 *cache, const int *slots, void *k, 
  *   for (a table much wider than the longest request is right, but a chunk may run slower); results are right for any value >= 1.
  *   ws: iso_attn_kv4_workspace bytes, zero-filled before its first use (every call leaves it ready for the next call of the same
  *   context, of any shape that fits).  Calls that may overlap in time, replays of a graph among them, need one each.
- *   q, out and ws must not overlap (ISO_ERR_SHAPE).
+ *   out and ws must not overlap one another or an input (ISO_ERR_SHAPE; of the table, the first entry is looked at).
  * Results do not depend on the order in which workgroups run.
  * Errors: NULL, n_seqs outside [1, 4096], total_rows, max_rows or max_pages < 1, total_rows * nq not below 2^31 (with
  * ISO_FLAG_SIMPLE_ATTN more than 2^26 - 4 rows or 65535 heads too), max_pages * page above 2^31 - 1024, q_stride (ISO_ERR_SHAPE), ws too small

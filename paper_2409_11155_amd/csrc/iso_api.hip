@@ -885,6 +885,13 @@ int check_rows(const iso_cfg &c, int T) {
     return ISO_OK;
 }
 
+// The cache's four buffers, for check_apart.
+struct Kv4Bytes { Bytes k, v, ks, vs; };
+Kv4Bytes kv4_bytes(const iso_cfg &c, const iso_kv4 &x) {
+    const size_t rows = (size_t)x.n_pages * x.page * c.n_kv_heads, codes = rows * (c.head_dim / 2), scales = rows * (c.head_dim / KV4_BLOCK);
+    return Kv4Bytes{{x.k, codes}, {x.v, codes}, {x.k_scale, scales}, {x.v_scale, scales}};
+}
+
 int check_kv4(const iso_kv4 *c) {
     if (!c) return fail(ISO_ERR_NULL, "cache is NULL");
     if (!c->k || !c->v || !c->k_scale || !c->v_scale) return fail(ISO_ERR_NULL, "the cache's k, v, k_scale and v_scale must be non-NULL");
@@ -1445,7 +1452,9 @@ int iso_rope_kv4_write(iso_ctx *ctx, void *qkv, void *q_out, const iso_kv4 *cach
         return fail(ISO_ERR_SHAPE, "qkv and q_out must be 16-byte aligned, positions and slots 4-byte");
     const iso_cfg &c = ctx->cfg;
     const size_t head = (size_t)T * c.head_dim * (c.dtype == ISO_F32 ? 4 : 2);
-    ISO_TRY(check_apart({{q_out, head * c.n_q_heads}}, {{qkv, head * (c.n_q_heads + 2 * c.n_kv_heads)}}));
+    const Kv4Bytes kb = kv4_bytes(c, *cache);
+    const Bytes rows{qkv, head * (c.n_q_heads + 2 * c.n_kv_heads)}, pos{positions, 4 * (size_t)T}, to{slots, 4 * (size_t)T};
+    ISO_TRY(check_apart({q_out ? Bytes{q_out, head * c.n_q_heads} : rows, kb.k, kb.v, kb.ks, kb.vs}, {q_out ? rows : Bytes{nullptr, 0}, pos, to}));
     ISO_TRY(check_device(ctx));
     LAUNCH_TRY(ISO_K_ROPE_KV, (hipStream_t)stream,
                iso_launch_kv4_write(c.dtype, qkv, q_out, *cache, positions, slots, ctx->rope_cos, ctx->rope_sin, c.max_seq, T, c.n_q_heads,
@@ -1459,8 +1468,11 @@ int iso_kv4_store(iso_ctx *ctx, const void *k, const void *v, const iso_kv4 *cac
     ISO_TRY(check_kv4(cache));
     ISO_TRY(check_rows(ctx->cfg, T));
     if (!aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 4)) return fail(ISO_ERR_SHAPE, "k and v must be 16-byte aligned, slots 4-byte");
-    ISO_TRY(check_device(ctx));
     const iso_cfg &c = ctx->cfg;
+    const size_t bytes = (size_t)T * c.n_kv_heads * c.head_dim * (c.dtype == ISO_F32 ? 4 : 2);
+    const Kv4Bytes kb = kv4_bytes(c, *cache);
+    ISO_TRY(check_apart({kb.k, kb.v, kb.ks, kb.vs}, {{k, bytes}, {v, bytes}, {slots, 4 * (size_t)T}}));
+    ISO_TRY(check_device(ctx));
     LAUNCH_TRY(ISO_K_QUANT, (hipStream_t)stream,
                iso_launch_kv4_store(c.dtype, k, v, *cache, slots, T, c.n_kv_heads, c.head_dim, (hipStream_t)stream), "kv4 store");
     return ISO_OK;
@@ -1474,7 +1486,8 @@ int iso_kv4_load(iso_ctx *ctx, const iso_kv4 *cache, const int *slots, void *k, 
     if (!aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 4)) return fail(ISO_ERR_SHAPE, "k and v must be 16-byte aligned, slots 4-byte");
     const iso_cfg &c = ctx->cfg;
     const size_t bytes = (size_t)T * c.n_kv_heads * c.head_dim * (c.dtype == ISO_F32 ? 4 : 2);
-    ISO_TRY(check_apart({{k, bytes}, {v, bytes}}, {}));
+    const Kv4Bytes kb = kv4_bytes(c, *cache);
+    ISO_TRY(check_apart({{k, bytes}, {v, bytes}}, {kb.k, kb.v, kb.ks, kb.vs, {slots, 4 * (size_t)T}}));
     ISO_TRY(check_device(ctx));
     LAUNCH_TRY(ISO_K_QUANT, (hipStream_t)stream,
                iso_launch_kv4_load(c.dtype, *cache, slots, k, v, T, c.n_kv_heads, c.head_dim, (hipStream_t)stream), "kv4 load");
@@ -1511,7 +1524,12 @@ int iso_attn_kv4(iso_ctx *ctx, const void *q, int q_stride, const iso_kv4 *cache
     if (!aligned(q, 16) || !aligned(out, 16) || !aligned(ws, 16) || !aligned(block_table, 4) || !aligned(row_start, 4) || !aligned(kv_len, 4))
         return fail(ISO_ERR_SHAPE, "q, out and ws must be 16-byte aligned, int buffers 4-byte");
     const size_t elt = c.dtype == ISO_F32 ? 4 : 2, row = (size_t)c.n_q_heads * c.head_dim;
-    ISO_TRY(check_apart({{out, elt * total_rows * row}, {ws, need}}, {{q, elt * ((size_t)(total_rows - 1) * q_stride + row)}}));
+    const Kv4Bytes kb = kv4_bytes(c, *cache);
+    const size_t seqs = 4 * (size_t)n_seqs;
+    // (the table's first entry: which others are read is known on the device, and a table as wide as a program's longest context need not
+    // have memory behind columns that no request reaches)
+    ISO_TRY(check_apart({{out, elt * total_rows * row}, {ws, need}}, {{q, elt * ((size_t)(total_rows - 1) * q_stride + row)}, kb.k, kb.v, kb.ks, kb.vs,
+                                                                      {block_table, 4}, {row_start, seqs + 4}, {kv_len, seqs}}));
     ISO_TRY(sk_status(ctx));
     ISO_TRY(check_device(ctx));
     const kv4_batch b{block_table, row_start, kv_len, max_pages, n_seqs, total_rows};

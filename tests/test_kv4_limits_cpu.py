@@ -59,3 +59,50 @@ for dt, nq, nkv, d in (("bf16", 1, 1, 128), ("bf16", 8, 1, 128), ("bf16", 13, 13
                 assert L.iso_attn_kv4(ctx._h, far[4], nq * d, c, far[6], 4, far[6], far[6], 1, rows, rows, far[5], far[7], n, None) == want, iso.last_error()
         log()
 """)
+
+
+def test_what_is_written_lies_apart_from_everything_else(fake):            # noqa: F811
+    """The cache, tables, positions and slots too, to the byte on both sides."""
+    run(fake, """
+L = iso.load()
+NKV, D, T, PAGE, PAGES = 2, 64, 8, 16, 4
+far = [(i + 1) << 40 for i in range(20)]
+for dt, e in (("bf16", 2), ("f32", 4)):
+    with iso.Context(iso.make_cfg(64, 4, NKV, D, 64, dt, 256)) as ctx:
+        h = ctx._h
+        codes, scales = PAGES * PAGE * NKV * D // 2, PAGES * PAGE * NKV * D // 32
+        n = ctx.attn_kv4_workspace(3, T)
+        size = dict(k=codes, v=codes, ks=scales, vs=scales, qkv=T * 8 * D * e, q=T * 4 * D * e, kr=T * NKV * D * e, vr=T * NKV * D * e, pos=4 * T, slots=4 * T,
+                    out=T * 4 * D * e, ws=n, table=4, start=16, lens=12)
+        at = dict(zip(size, far))
+        def cache(a):
+            return ctypes.byref(iso.IsoKv4(a["k"], a["v"], a["ks"], a["vs"], PAGES, PAGE))
+        calls = {
+            "write": lambda a: L.iso_rope_kv4_write(h, a["qkv"], a["q"], cache(a), a["pos"], a["slots"], T, None),
+            "write in place": lambda a: L.iso_rope_kv4_write(h, a["qkv"], None, cache(a), a["pos"], a["slots"], T, None),
+            "store": lambda a: L.iso_kv4_store(h, a["kr"], a["vr"], cache(a), a["slots"], T, None),
+            "load": lambda a: L.iso_kv4_load(h, cache(a), a["slots"], a["kr"], a["vr"], T, None),
+            "attn": lambda a: L.iso_attn_kv4(h, a["q"], 4 * D, cache(a), a["table"], 4, a["start"], a["lens"], 3, T, T, a["out"], a["ws"], n, None)}
+        four = ("k", "v", "ks", "vs")
+        outs = {"write": ("q", *four), "write in place": ("qkv", *four), "store": four, "load": ("kr", "vr"), "attn": ("out", "ws")}
+        ins = {"write": ("qkv", "pos", "slots"), "write in place": ("pos", "slots"), "store": ("kr", "vr", "slots"), "load": (*four, "slots"),
+               "attn": (*four, "q", "table", "start", "lens")}
+        for name, call in calls.items():
+            assert call(at) == 0, iso.last_error()
+            log()
+            for o in outs[name]:
+                for x in outs[name] + ins[name]:
+                    if x == o:
+                        continue
+                    align = 4 if x in ("pos", "slots", "table", "start", "lens") else 16
+                    up = -(-size[o] // align) * align              # x behind o, and its last byte in front of it
+                    for place, want in ((at[o], -2), (at[o] + up - align, -2), (at[o] + up, 0), (at[o] - (size[x] - align) // align * align, -2),
+                                        (at[o] - -(-size[x] // align) * align, 0)):
+                        if up - align >= size[o] and place == at[o] + up - align:
+                            continue
+                        assert call({**at, x: place}) == want, (name, o, x, place - at[o], iso.last_error())
+                        assert want == 0 or "overlap" in iso.last_error()
+            assert all(l[0] == "kernel" for l in log())
+        same = dict(at, vr=at["kr"])                             # inputs may be one another
+        assert calls["store"](same) == 0 and calls["load"](dict(at, v=at["k"], vs=at["ks"])) == 0 and calls["attn"](dict(at, v=at["k"], start=at["lens"])) == 0
+""")
