@@ -341,6 +341,25 @@ def _ptr(t) -> Optional[int]:
     raise ValueError("libiso takes contiguous buffers")
 
 
+_INT32 = {"i32"}                                        # and what torch calls it, once seen
+
+
+def _ints(t) -> Optional[int]:
+    """Address of a buffer of 32-bit integers.  One that says it holds anything else is refused (torch makes indices of 64 bits)."""
+    if t is None:
+        return None
+    try:
+        if t.dtype in _INT32 and t.is_contiguous():
+            return t.data_ptr()
+        if str(t.dtype) == "torch.int32":
+            _INT32.add(t.dtype)
+        elif t.dtype not in _INT32:
+            raise ValueError(f"lengths, tables, positions and slots are 32-bit integers, not {t.dtype}")
+    except AttributeError:                              # an address
+        pass
+    return _ptr(t)
+
+
 def copy_d2h_async(dst: "PinnedArray", src: "DeviceArray", nbytes: int, stream) -> None:
     """Asynchronous device-to-host copy of the first nbytes of src into pinned memory, in `stream`."""
     _check(load().iso_copy_d2h_async(dst.ptr, src.ptr, int(nbytes), _stream_handle(stream)))
@@ -377,6 +396,9 @@ class Kv4Cache:
         if len(shapes[0]) != 4 or shapes[0] != shapes[1] or shapes[2] != shapes[3] or shapes[0][:3] != shapes[2][:3] or \
                 shapes[0][2] != page or shapes[2][3] * 16 != shapes[0][3]:
             raise ValueError(f"not the buffers of a 4-bit cache with pages of {page} tokens: {shapes}")
+        for a in (k, v, k_scale, v_scale):
+            if (DTYPE_BYTES[a.dtype] if a.dtype in _NP_STORAGE else a.element_size()) != 1:
+                raise ValueError(f"the buffers of a 4-bit cache are bytes, not {a.dtype}")
         self.page, self.n_pages, self.nkv, self.head_dim = page, shapes[0][0], shapes[0][1], 2 * shapes[0][3]
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale      # kept alive
         self.handle = IsoKv4(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), self.n_pages, page)
@@ -534,19 +556,19 @@ class Context:
 
     def block_tables(self, cached, fresh, n_seqs: int, page: int, free_pages, n_free: int, free_head, block_table, max_pages: int, row_start,
                      kv_len, positions, slots, max_rows: int, free_next, stream=None) -> None:
-        _check(self._lib.iso_block_tables(self._h, _ptr(cached), _ptr(fresh), n_seqs, page, _ptr(free_pages), n_free, _ptr(free_head),
-                                          _ptr(block_table), max_pages, _ptr(row_start), _ptr(kv_len), _ptr(positions), _ptr(slots),
-                                          max_rows, _ptr(free_next), _stream_handle(stream)))
+        _check(self._lib.iso_block_tables(self._h, _ints(cached), _ints(fresh), n_seqs, page, _ints(free_pages), n_free, _ints(free_head),
+                                          _ints(block_table), max_pages, _ints(row_start), _ints(kv_len), _ints(positions), _ints(slots),
+                                          max_rows, _ints(free_next), _stream_handle(stream)))
 
     def rope_kv4_write(self, qkv, q_out, cache: Kv4Cache, positions, slots, T: int, stream=None) -> None:
-        _check(self._lib.iso_rope_kv4_write(self._h, _ptr(qkv), _ptr(q_out), self._kv4(cache), _ptr(positions), _ptr(slots), T,
+        _check(self._lib.iso_rope_kv4_write(self._h, _ptr(qkv), _ptr(q_out), self._kv4(cache), _ints(positions), _ints(slots), T,
                                             _stream_handle(stream)))
 
     def kv4_store(self, k, v, cache: Kv4Cache, slots, T: int, stream=None) -> None:
-        _check(self._lib.iso_kv4_store(self._h, _ptr(k), _ptr(v), self._kv4(cache), _ptr(slots), T, _stream_handle(stream)))
+        _check(self._lib.iso_kv4_store(self._h, _ptr(k), _ptr(v), self._kv4(cache), _ints(slots), T, _stream_handle(stream)))
 
     def kv4_load(self, cache: Kv4Cache, slots, k, v, T: int, stream=None) -> None:
-        _check(self._lib.iso_kv4_load(self._h, self._kv4(cache), _ptr(slots), _ptr(k), _ptr(v), T, _stream_handle(stream)))
+        _check(self._lib.iso_kv4_load(self._h, self._kv4(cache), _ints(slots), _ptr(k), _ptr(v), T, _stream_handle(stream)))
 
     def attn_kv4_workspace(self, n_seqs: int, total_rows: int) -> int:
         n = ctypes.c_size_t()
@@ -555,5 +577,5 @@ class Context:
 
     def attn_kv4(self, q, q_stride: int, cache: Kv4Cache, block_table, max_pages: int, row_start, kv_len, n_seqs: int, total_rows: int,
                  max_rows: int, out, ws, ws_bytes: int, stream=None) -> None:
-        _check(self._lib.iso_attn_kv4(self._h, _ptr(q), q_stride, self._kv4(cache), _ptr(block_table), max_pages, _ptr(row_start),
-                                      _ptr(kv_len), n_seqs, total_rows, max_rows, _ptr(out), _ptr(ws), ws_bytes, _stream_handle(stream)))
+        _check(self._lib.iso_attn_kv4(self._h, _ptr(q), q_stride, self._kv4(cache), _ints(block_table), max_pages, _ints(row_start),
+                                      _ints(kv_len), n_seqs, total_rows, max_rows, _ptr(out), _ptr(ws), ws_bytes, _stream_handle(stream)))

@@ -106,3 +106,71 @@ for dt, e in (("bf16", 2), ("f32", 4)):
         same = dict(at, vr=at["kr"])                             # inputs may be one another
         assert calls["store"](same) == 0 and calls["load"](dict(at, v=at["k"], vs=at["ks"])) == 0 and calls["attn"](dict(at, v=at["k"], start=at["lens"])) == 0
 """)
+
+
+def test_index_buffers_of_another_type(fake):                  # noqa: F811
+    """Every length, table, position and slot of every call; torch's tensors are known by the name of their type."""
+    run(fake, """
+class Type:
+    def __init__(self, name):
+        self.name = name
+    def __repr__(self):
+        return self.name
+class Tensor:                                                    # what the binding asks a tensor for
+    def __init__(self, dtype, ptr, contiguous=True):
+        self.dtype, self.ptr, self.contiguous = dtype, ptr, contiguous
+    def is_contiguous(self):
+        return self.contiguous
+    def data_ptr(self):
+        return self.ptr
+i32, i64 = Type("torch.int32"), Type("torch.int64")
+with iso.Context(iso.make_cfg(64, 4, 2, 64, 64, "bf16", 256)) as ctx:
+    cache = ctx.kv4_cache(4, 16)
+    a, b = (iso.DeviceArray((8, 8, 64), "bf16") for _ in range(2))
+    n = ctx.attn_kv4_workspace(2, 8)
+    ws = iso.DeviceArray((n,), "u8")
+    calls = {"block_tables": (dict(cached=1, fresh=1, n_seqs=2, page=16, free_pages=1, n_free=4, free_head=1, block_table=1, max_pages=4, row_start=1, kv_len=1,
+                                   positions=1, slots=1, max_rows=8, free_next=1), "cached fresh free_pages free_head block_table row_start kv_len positions slots free_next"),
+             "rope_kv4_write": (dict(qkv=a, q_out=b, cache=cache, positions=1, slots=1, T=8), "positions slots"),
+             "kv4_store": (dict(k=a, v=b, cache=cache, slots=1, T=8), "slots"),
+             "kv4_load": (dict(k=a, v=b, cache=cache, slots=1, T=8), "slots"),
+             "attn_kv4": (dict(q=a, q_stride=256, cache=cache, block_table=1, max_pages=4, row_start=1, kv_len=1, n_seqs=2, total_rows=8, max_rows=8, out=b, ws=ws, ws_bytes=n),
+                          "block_table row_start kv_len")}
+    for name, (kw, ints) in calls.items():
+        ints = ints.split()
+        bufs = {x: iso.DeviceArray((64,), "i32") for x in ints}
+        f = getattr(ctx, name)
+        f(**{**kw, **bufs})
+        f(**{**kw, **{x: y.ptr for x, y in bufs.items()}})       # addresses
+        for _ in range(2):
+            f(**{**kw, **{x: Tensor(i32, y.ptr) for x, y in bufs.items()}})
+        log()
+        for x in ints:
+            for bad in (Tensor(i64, bufs[x].ptr), Tensor(Type("torch.float32"), bufs[x].ptr), Tensor(i32, bufs[x].ptr, False), iso.DeviceArray((64,), "f32"),
+                        iso.DeviceArray((256,), "u8")):
+                try:
+                    f(**{**kw, **bufs, x: bad})
+                    assert False, (name, x, bad.dtype)
+                except ValueError as e:
+                    assert ("32-bit integers" if bad.dtype is not i32 else "contiguous") in str(e)
+        assert not [l for l in log() if l[0] == "kernel"]
+    ctx.block_tables(bufs["kv_len"], bufs["row_start"], 1, 16, None, 0, None, *(x if isinstance(x, int) else iso.DeviceArray((64,), "i32") for x in ("t", 4, "s", "l", "p", "q", 8, "n")))
+    try:
+        iso.Kv4Cache(16, *(iso.DeviceArray((4, 2, 16, w), "bf16") for w in (32, 32, 2, 2)))
+        assert False
+    except ValueError as e:
+        assert "bytes" in str(e)
+""")
+
+
+def test_torch_tensors_of_32_bits_only():
+    import pytest
+    torch = pytest.importorskip("torch")
+    import paper_2409_11155_amd as iso
+    t = torch.zeros(5, dtype=torch.int32)
+    for _ in range(2):
+        assert iso._ints(t) == t.data_ptr()
+    for bad in (torch.zeros(5, dtype=torch.int64), torch.zeros(5), torch.zeros(5, dtype=torch.int16), t[::2]):
+        with pytest.raises(ValueError):
+            iso._ints(bad)
+    assert iso._ints(None) is None and iso._ints(4096) == 4096
