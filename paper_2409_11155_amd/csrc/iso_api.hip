@@ -910,8 +910,11 @@ int check_kv4(const iso_kv4 *c) {
 //                     128 / 256 rows of 32768                85 / 98 and 68 / 115;             16 of 8192    47 and 20
 //   8 heads over 1:   2048 rows of 2048 / 8192 / 32768       34 / 86 / 321 and 33 / 111 / 416
 //   13 heads over 13: 640 rows of 2048 / 4096, 2047 of 2047  34 / 42 / 38 and 28 / 41 / 45
-// Of several requests the shorter ones stay with the line, which costs a second launch: 22 single tokens (16 heads over 2) and
+// Of several requests those of up to SHORT_PAIRS pairs of a key head stay with the line.  Where max_rows allows no others there is no second
+// launch: it would find nothing to do (13 heads over 13, 2 x 400 rows of 2000 keys in a wide table 33.4 us with it, 31.2 without; 32 heads
+// of 64 over 8, 2 x 250 rows of 8000 keys 87 and 84).  22 single tokens (16 heads over 2) and
 //   2 x 512 rows of up to 6000 / 20000 keys  59 / 109 and 51 / 117;  4 x 512 of up to 8192  103 and 116;  1024 of up to 6000  49 and 35
+constexpr int SHORT_PAIRS = 1023;
 struct Kv4Launch {
     bool line, rows;
     int most;                      // pairs of (row, query head of a key head) up to which a request belongs to the line
@@ -923,9 +926,10 @@ Kv4Launch kv4_launch(const iso_cfg &c, int n_seqs, int total_rows, int max_rows,
     auto many = [&](int rows) { return can && (long long)rows * c.n_q_heads >= 4096; };
     const long long work = (long long)total_rows * c.n_q_heads * keys;
     Kv4Launch l;
-    l.rows = n_seqs == 1 ? many(total_rows) && work > 1ll << 25 : many(std::min(max_rows, total_rows)) && work > 1ll << 27;
+    const int rows = n_seqs == 1 ? total_rows : std::min(max_rows, total_rows);
+    l.rows = many(rows) && work > (n_seqs == 1 ? 1ll << 25 : 1ll << 27) && (n_seqs == 1 || (long long)rows * (c.n_q_heads / c.n_kv_heads) > SHORT_PAIRS);
     l.line = !l.rows || n_seqs > 1;
-    l.most = !l.rows ? 0x7fffffff : l.line ? 1023 : 0;
+    l.most = !l.rows ? 0x7fffffff : l.line ? SHORT_PAIRS : 0;
     l.line_bytes = align_up(iso_attn_kv4_ws_bytes(c.dtype, c.n_kv_heads, c.head_dim, ncu), 256);
     l.rows_bytes = many(total_rows) ? iso_attn_kv4_rows_ws_bytes(c.n_kv_heads, c.head_dim, ncu) : 0;
     return l;

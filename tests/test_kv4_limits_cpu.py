@@ -174,3 +174,28 @@ def test_torch_tensors_of_32_bits_only():
         with pytest.raises(ValueError):
             iso._ints(bad)
     assert iso._ints(None) is None and iso._ints(4096) == 4096
+
+
+def test_no_launch_for_requests_that_there_cannot_be(fake):    # noqa: F811
+    """Of several requests the tiles of 128 rows take those of more than 1023 (row, query head) pairs of a KEY head.  Where max_rows allows
+    none, the launch beside the line is left out, and the line takes requests of any size (max_rows is a hint)."""
+    run(fake, """
+def kernels(nq, nkv, d, n_seqs, rows, most, keys=1 << 16):
+    with iso.Context(iso.make_cfg(64, nq, nkv, d, 64, "bf16", 256)) as ctx:
+        cache = ctx.kv4_cache(4, 16)
+        i = iso.DeviceArray((n_seqs * keys // 16,), "i32")
+        q, out = (iso.DeviceArray((rows, nq, d), "bf16") for _ in range(2))
+        n = ctx.attn_kv4_workspace(n_seqs, rows)
+        ws = iso.DeviceArray((n,), "u8")
+        log()
+        ctx.attn_kv4(q, nq * d, cache, i, keys // 16, i, i, n_seqs, rows, most, out, ws, n)
+        return ["rows" if "rows" in l[2].split()[0] else "line" for l in log() if l[0] == "kernel"]
+for nq, nkv, d in ((13, 13, 128), (64, 64, 64), (66, 22, 128), (16, 2, 128), (8, 1, 128), (32, 8, 64)):
+    G = nq // nkv
+    first = 1023 // G + 1                                        # rows of the first request that is long enough
+    assert kernels(nq, nkv, d, 2, 2 * first - 2, first - 1) == ["line"], (nq, nkv)
+    assert kernels(nq, nkv, d, 2, 2 * first, first) == (["line", "rows"] if first * nq >= 4096 else ["line"]), (nq, nkv)
+    assert kernels(nq, nkv, d, 2, first, 2 ** 31 - 1) == (["line", "rows"] if first * nq >= 4096 else ["line"]), (nq, nkv)
+    one = 4096 // nq + 1                                         # a single request has one launch, whatever its pairs of a key head
+    assert kernels(nq, nkv, d, 1, one, one) == ["rows"] and kernels(nq, nkv, d, 1, one - 2, one) == ["line"], (nq, nkv)
+""")
