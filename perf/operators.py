@@ -33,6 +33,7 @@ TORCH = {"f32": torch.float32, "bf16": torch.bfloat16}
 LEVELS = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
 BLOCK = 32
 ROPE_BASE = 10000.0
+WRITTEN = 8320                           # no case writes a token behind it
 
 
 def listed():
@@ -116,13 +117,6 @@ def lengths(case):
     return kv, fresh
 
 
-def span(case):
-    """Positions that a context has to know."""
-    if case["op"] == "store":
-        return case["T"]
-    return max(64, case["hi"] + 1)
-
-
 # ------------------------------------------------------------------------------------------------ the format, in plain steps
 
 def encode(x):
@@ -184,12 +178,17 @@ def _cache(n_pages, nkv, page, d):
     return {"k": z(d // 2), "v": z(d // 2), "k_scale": z(d // BLOCK), "v_scale": z(d // BLOCK)}
 
 
-@functools.lru_cache(maxsize=None)
 def _context(heads, positions):
-    """The context that a serving program keeps; the operators use nothing of it but the heads, the type and the rotary table."""
+    """The context that a serving program keeps: one for each shard, with a rotary table for the positions that are written (the other
+    calls use nothing of it but the heads and the type)."""
+    return _contexts(heads, positions, torch.cuda.current_stream())
+
+
+@functools.lru_cache(maxsize=None)
+def _contexts(heads, positions, stream):
     import paper_2409_11155_amd as iso
     nq, nkv, d, dt = heads
-    return iso.Context(iso.make_cfg(64, nq, nkv, d, 64, dt, positions, rope_base=ROPE_BASE), stream0=torch.cuda.current_stream())
+    return iso.Context(iso.make_cfg(64, nq, nkv, d, 64, dt, positions, rope_base=ROPE_BASE), stream0=stream)
 
 
 def prepare(case, seed):
@@ -229,7 +228,7 @@ def prepare(case, seed):
             st["q"] = torch.zeros((T, nq, d), device=dev, dtype=TORCH[dt])
         if own:
             import paper_2409_11155_amd as iso
-            st["ctx"] = _context(heads, span(case))
+            st["ctx"] = _context(heads, 64 if case["op"] == "store" else WRITTEN)
             st["kv4"] = iso.Kv4Cache(page=page, **st["cache"])
         return st
     kv, fresh = lengths(case)
@@ -248,7 +247,7 @@ def prepare(case, seed):
           "q": normal(rows, nq, d), "out": torch.zeros((rows, nq, d), device=dev, dtype=TORCH[dt]), "rows": rows, "most": max(fresh), "longest": max(kv)}
     if own:
         import paper_2409_11155_amd as iso
-        st["ctx"] = _context(heads, span(case))
+        st["ctx"] = _context(heads, 64)
         st["kv4"] = iso.Kv4Cache(page=page, **cache)
         bytes_ = st["ctx"].attn_kv4_workspace(len(kv), rows)
         st["ws"] = torch.zeros(bytes_, device=dev, dtype=torch.uint8)
