@@ -318,8 +318,11 @@ int iso_gemm_fp8(iso_ctx *ctx, const void *a8, const float *sa, const void *w8, 
  *   Format.  Blocks of 32 neighbouring elements of a head share a scale 2^(s-127), s one byte; an element is a sign and one of
  *   0, 0.5, 1, 1.5, 2, 3, 4, 6 (E2M1: sign, two exponent bits, one fraction bit), two elements a byte, the first in the low four
  *   bits.  Writing a block x: e = least integer with max|x| <= 7 * 2^e, not below -125 nor above 125; s = e + 127; each element the
- *   nearest of the values times 2^e, ties to the even code.  An element is off by at most 2^e, i.e. less than 2/7 of the block's
- *   largest.  A block with a NaN or an infinity gets s = 255 and stands for 32 NaN.
+ *   nearest of the values times 2^e, ties to the even code.  Where 7 * 2^-126 < max|x| <= 7 * 2^125 an element is off by at most
+ *   2^e, i.e. less than 2/7 of the block's largest.  Beyond, e is cut: larger elements become 6 * 2^125, off by up to 2^126 (a rotated
+ *   key can be larger than its type's largest number, and off by more); in a smaller block an element is off by at most 2^-126, and one of
+ *   up to 2^-127 becomes zero.
+ *   A block with a NaN or an infinity gets s = 255 and stands for 32 NaN.
  *   (Bytes 0, 1, 253 and 254 are not written, and what they stand for is not defined.)
  *   Layout.  k, v [n_pages, nkv, page, d/2] bytes; k_scale, v_scale [n_pages, nkv, page, d/32] bytes.  A token's slot is its page's
  *   number * page + its place in the page.  Both context types (ISO_F32, ISO_BF16) read and write it; nothing in it depends on the

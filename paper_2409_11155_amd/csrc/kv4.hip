@@ -142,7 +142,7 @@ __device__ __forceinline__ float round_to_odd(double x) {
 
 // Codes and scale of the block that four neighbouring lanes hold: e = least integer with max|x| <= 7 * 2^e.  (7 and not 6: what lies
 // above 6 * 2^e is then off by at most 2^e, no more than between 4 and 6.)  The least e is -125, for every value to be a normal bf16
-// number, the largest 125, for none to be infinite.  Ties go to the even code, what is above 6 * 2^e to 6: as the instruction does.
+// number, the largest 125, for none to be infinite; there smaller elements go to zero and larger ones to 6 * 2^125.  Ties go to the even code, what is above 6 * 2^e to 6: as the instruction does.
 __device__ __forceinline__ unsigned encode8(const float (&x)[8], unsigned *scale) {
     unsigned top = 0;
 #pragma unroll

@@ -199,3 +199,25 @@ for nq, nkv, d in ((13, 13, 128), (64, 64, 64), (66, 22, 128), (16, 2, 128), (8,
     one = 4096 // nq + 1                                         # a single request has one launch, whatever its pairs of a key head
     assert kernels(nq, nkv, d, 1, one, one) == ["rows"] and kernels(nq, nkv, d, 1, one - 2, one) == ["line"], (nq, nkv)
 """)
+
+
+def test_how_far_an_element_is_off_over_the_whole_range():
+    """2^e between the ends of the scale; beyond them 2^126 above (what is larger than 6 * 2^125 becomes that) and 2^-126 below."""
+    import numpy as np
+    from oracle import kv4_oracle as ko
+    rng = np.random.default_rng(0)
+    top = np.exp2(rng.integers(-150, 128, 20000).astype(float)) * (1 + rng.random(20000) * (1 - 2.0 ** -24))
+    top[:8] = [7 * 2.0 ** -126, np.nextafter(7 * 2.0 ** -126, 1), 7 * 2.0 ** 125, np.nextafter(7 * 2.0 ** 125, np.inf), 2.0 ** 128 * (1 - 2.0 ** -24), 2.0 ** -127, 2.0 ** -149, 3.4e38]
+    x = rng.uniform(-1, 1, (20000, 32)) * top[:, None]
+    x[:, 5] = top
+    codes, scales = ko.encode(x)
+    off = np.abs(x - ko.decode(codes, scales)).max(1)
+    small, large = top <= 7 * 2.0 ** -126, top > 7 * 2.0 ** 125
+    inside = ~small & ~large
+    assert small.sum() > 1000 and large.sum() > 10 and inside.sum() > 10000
+    assert (off[inside] <= np.exp2(scales[inside, 0] - 127.0)).all() and (off[inside] < 2 / 7 * top[inside]).all()
+    assert (scales[large] == 252).all() and (off[large] <= 2.0 ** 126).all() and off[large].max() > 1.9 * 2.0 ** 125
+    assert (ko.decode(codes, scales)[large, 5] == 6 * 2.0 ** 125).all()
+    assert (scales[small] == 2).all() and (off[small] <= 2.0 ** -126).all()
+    gone = top <= 2.0 ** -127
+    assert (ko.decode(codes, scales)[gone] == 0).all() and gone.sum() > 1000
