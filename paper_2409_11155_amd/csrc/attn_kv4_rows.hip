@@ -21,16 +21,12 @@
 
 namespace {
 
-typedef unsigned long long u64;
 constexpr int BM = 128, BN = 64, THREADS = 256;
 constexpr u64 SETUP = 256;             // what a row tile's start and end cost, in keys
 constexpr int MIN_SHARE = 512;           // keys of a share, at least
 constexpr int PIECES = 32;               // shares that a row tile is cut into, at most (and one more where it begins inside one)
-constexpr int COHERENT = 1 | 16;         // buffer cache policy sc0 | sc1: system scope, bypasses the XCD-local L2
 template <int D> constexpr int part_bytes() { return D / 8 * THREADS * 16 + THREADS * 8; }      // D / 8 float4 and (maximum, sum) a lane
 
-typedef __bf16 bf16x4_v __attribute__((ext_vector_type(4)));
-typedef unsigned u32x2_v __attribute__((ext_vector_type(2)));
 struct rows_args {
     const bf16_t *q;
     bf16_t *out;
@@ -41,11 +37,6 @@ struct rows_args {
     int q_stride, nq, nkv, G, toks;      // toks: tokens of a row tile
     int most;                            // requests of at most this many (row, head) pairs belong to another launch
 };
-
-typedef const __attribute__((address_space(4))) int *scalar_ints;
-__device__ __forceinline__ scalar_ints scalar(const int *p) { return (scalar_ints)(uintptr_t)p; }
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ u64 uniform(u64 x) { return (u64)(unsigned)uniform((int)x) | (u64)(unsigned)uniform((int)(x >> 32)) << 32; }
 
 // As in attn_bf16_dtl.hip: the transposing read as an instruction, and the wait for all but the N youngest LDS reads.
 template <int OFF> __device__ __forceinline__ bf16x4_v read_tr(uint32_t addr) {
@@ -60,14 +51,6 @@ __device__ __forceinline__ float half_swap_max(float v) {
     const unsigned u = __float_as_uint(v);
     const u32x2_v r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ bf16x8_t unpack8(unsigned w, float scale) {
-    const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
-    const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
-    return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t beyond(unsigned char *p, u64 at) {
-    return __builtin_amdgcn_make_buffer_rsrc((void *)(p + at), 0, -1, 0x00020000);
 }
 
 template <int D> __global__ __launch_bounds__(THREADS, 2) void attn_kv4_rows_kernel(rows_args a) {

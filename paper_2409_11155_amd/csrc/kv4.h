@@ -50,3 +50,27 @@ template <typename P> __device__ __forceinline__ int kv4_keys_of(P kv_len, int m
     const long long cap = (long long)max_pages << page_shift;
     return (int)min((long long)max(0, kv_len[i]), cap);
 }
+
+// ---- what both tiled attention kernels use
+typedef unsigned long long u64;
+typedef __bf16 bf16x4_v __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2_v __attribute__((ext_vector_type(2)));
+constexpr int COHERENT = 1 | 16;      // buffer cache policy sc0 | sc1: system scope, bypasses the XCD-local L2
+
+// Eight elements of a code word (exact).
+__device__ __forceinline__ bf16x8_t unpack8(unsigned w, float scale) {
+    const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
+    const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
+    return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+// Wave-uniform values are made scalar explicitly, and what is read at a uniform place is read by the scalar unit: vector loads come
+// back in order, so a page number among them would have to wait for the codes requested before it.
+typedef const __attribute__((address_space(4))) int *scalar_ints;
+__device__ __forceinline__ scalar_ints scalar(const int *p) { return (scalar_ints)(uintptr_t)p; }
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ u64 uniform(u64 x) { return (u64)(unsigned)uniform((int)x) | (u64)(unsigned)uniform((int)(x >> 32)) << 32; }
+// Buffer from p + at on: a lane's address needs no addition in a vector register.  (`at` is not taken as the scalar offset: that one counts
+// in the comparison with the buffer's size, which cannot be more than 4 GB.)
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t beyond(unsigned char *p, u64 at) {
+    return __builtin_amdgcn_make_buffer_rsrc((void *)(p + at), 0, -1, 0x00020000);
+}
