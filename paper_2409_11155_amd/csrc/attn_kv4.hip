@@ -117,7 +117,7 @@ __device__ __forceinline__ u64 lane_of(u64 x, int lane) {
 template <typename T, int D, int RT>
 __global__ __launch_bounds__(THREADS, wg_per_cu(sizeof(T), D, RT)) void attn_kv4_kernel(line_args a) {
     constexpr int NP = sizeof(T) == 4 ? 3 : 1;               // bf16 terms of a query element ...
-    constexpr int NV = sizeof(T) == 4 ? 3 : kv4_terms(D);    // ... and of a probability
+    constexpr int NV = sizeof(T) == 4 ? 3 : kv4_terms(D, 16 * RT);    // ... and of a probability
     constexpr int ROWS = 16 * RT;
     constexpr int WPL = D / 32;              // code words (8 elements) a lane takes of a key
     constexpr int RB = 2 * D;                // bytes of an unpacked row

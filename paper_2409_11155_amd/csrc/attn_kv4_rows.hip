@@ -56,7 +56,7 @@ __device__ __forceinline__ float half_swap_max(float v) {
 template <int D> __global__ __launch_bounds__(THREADS, 2) void attn_kv4_rows_kernel(rows_args a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int WPL = D / 32;                  // code words (8 elements) a lane takes of a key: a quarter of its head
-    constexpr int NV = kv4_terms(D);             // bf16 terms of a probability
+    constexpr int NV = kv4_terms(D, BM);             // bf16 terms of a probability
     constexpr int ROW_B = 2 * D, TILE_B = BN * ROW_B, STAGE_B = 2 * TILE_B;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     __shared__ u64 nan_v[2][4];                  // per stage and loading wave: V blocks that are NaN (masked tiles only)

@@ -8,13 +8,15 @@ constexpr int KV4_BLOCK = 32;
 constexpr int KV4_MAX_SEQS = 4096;      // requests in one call: their prefix sums are kept in LDS
 constexpr int KV4_MAX_KEYS = 0x7fffffff - 1023;      // tokens that a request's table has room for: key counters run up to 300 past the last one
 
-// bf16 terms of a probability in the product with V (bf16 contexts; the probabilities' sum keeps 24 bits).  Heads of 64: the nearest and
-// the nearest of what is left, 16 bits, as in the attention over rows (attn_bf16_dtl.hip): results are as far from 64 bits as the rounding
-// of the output alone, 1.66e-3 of their size; with one term 2.1e-3.  Heads of 128: one, as there, 2.1e-3.  What the second term costs (us, one
-// and two): heads of 64, 32 over 8, 48 x 2 rows over 300 to 8192 keys 20.6 and 21.6, 500 rows of 2500 27 and 31, 2048 of 2048 40 and 47;
-// heads of 128: 40 single tokens of 13 heads 44.3 and 44.7, 2 x 509 rows and 22 tokens of 16 heads over 2 37.5 and 42.4, 2048 rows over
-// 32768 keys of 8 heads over 1 267 and 364 (its registers do not hold them).
-constexpr int kv4_terms(int d) { return d == 64 ? 2 : 1; }
+// bf16 terms of a probability in the product with V, in tiles of so many (row, head) pairs (bf16 contexts; the probabilities' sum keeps 24
+// bits).  Two are the nearest and the nearest of what is left, 16 bits: results are then as far from 64 bits as the rounding of the output
+// alone, 1.66e-3 of their size; with one term 2.1e-3.  Heads of 64: two, as in the attention over rows (attn_bf16_dtl.hip).  Heads of 128: there
+// it is one; here two where they cost next to nothing, in tiles of 16 pairs, which wait for the cache's bytes.  Times of one and two (us):
+//   heads of 64, 32 over 8:  48 x 2 rows over 300 to 8192 keys 20.6 and 21.6,  500 rows of 2500 27 and 31,  2048 of 2048 40 and 47
+//   heads of 128, tiles of 16:  40 single tokens, 13 heads over 13, 500 to 8192 keys 44.3 and 44.7,  one of 131072, 8 over 1, 16.6 and 16.9
+//     512 rows of 2000, 13 over 13, 26.0 and 27.5;
+//   tiles of 32:  2 x 509 rows and 22 tokens, 16 over 2, 700 to 6000 keys 37.5 and 42.4;  of 128:  2048 of 32768, 8 over 1, 267 and 364 (spilled)
+constexpr int kv4_terms(int d, int tile) { return d == 64 || tile == 16 ? 2 : 1; }
 
 // Device view of an iso_kv4.  Strides in bytes; a page holds every kv head's tokens, a head's tokens are contiguous.
 struct kv4_view {

@@ -1,5 +1,5 @@
-"""Attention over the 4-bit cache with heads of 64 in bf16: as exact as the framework's attention over rows, which carries a probability
-as two bf16 terms.
+"""Attention over the 4-bit cache in bf16 where a probability is two bf16 terms: heads of 64, as exact as the framework's attention over
+rows, which has two there as well, and tiles of 16 (row, head) pairs.
 
 Bound per element, with A the probability-weighted mean of |v| and N the number of keys:
   2^-8 |out|                   the result is rounded once
@@ -63,3 +63,16 @@ def test_pages_are_attended_to_as_exactly_as_rows(kv, fresh):
     mine, theirs = (float(np.sqrt(((x - ref) ** 2).mean() / (ref ** 2).mean())) for x in (got, base))
     print(f"{kv} {fresh}: {mine:.4e} {theirs:.4e}")
     assert mine <= theirs * (1.02 if fresh > 400 else 1.2)
+
+
+@pytest.mark.parametrize("heads", [(8, 1), (13, 13), (16, 2), (3, 1)])
+@pytest.mark.parametrize("kv,fresh,page", [([1], [1], 16), ([5, 900, 1, 2049, 333, 64], [1] * 6, 64), ([20000], [1], 64), ([700, 41, 1300], [2, 3, 5], 128),
+                                           ([2000] * 40, [1] * 40, 64)])
+def test_tiles_of_sixteen_keep_sixteen_bits_for_heads_of_128_too(heads, kv, fresh, page):
+    nq, nkv = heads
+    table, row_start, n_pages = batch(kv, fresh, page, seed=2)
+    codes, scales = fill(n_pages, nkv, page, 128, 3, table, kv)
+    q = iso_inputs.randn((int(row_start[-1]), nq, 128), seed=9, dtype="bf16")
+    with make_ctx(nq, nkv, 128, "bf16") as ctx:
+        got = f64(attend(ctx, q, device_cache(codes, scales, page), table, row_start, kv, "bf16", nq, 128), "bf16")
+    check_two_terms(got, f64(q, "bf16"), ko.decode(codes[0], scales[0]), ko.decode(codes[1], scales[1]), table, page, row_start, kv, nq // nkv, n_pages)
