@@ -7,7 +7,7 @@
 //   * K goes from the page into the registers that the product wants: the four lanes of a key take a quarter of its head each, 16 (8)
 //     bytes, and element order inside the head is free as long as q is read in the same one.  No LDS.
 //   * V has to be transposed: a wave writes its 32 unpacked rows to LDS (its own 8 KB, no barrier) and reads them back with
-//     ds_read_b64_tr_b16.  16-byte chunks are XOR-swizzled by the row (heads of 128: the LDS works in 29 % of the cycles, a fifth of that
+//     ds_read_b64_tr_b16.  16-byte chunks are XOR-swizzled by the row (heads of 128: the LDS works in 23 % of the cycles, a fifth of that
 //     on bank conflicts).
 //   * RT = 2: what is unpacked once serves two blocks of 16 rows.  The second one is passed over where the tile does not reach it.
 //   * T = float: q and the probabilities are cut into three bf16 terms that add up to all 24 bits (K and V have two): three products.
@@ -21,12 +21,14 @@
 // back to zero.  Nobody waits for anybody.  The shares are computed on the device from the lengths there: a captured step keeps its balance
 // as the requests grow.
 //
-// Measured (bf16): 40 single tokens over 500 to 8192 keys, 13 heads of 128, 43.4 us, 4.2 TB/s of the cache (a large copy reaches 4.9);
-// 48 x 2 rows over 300 to 8192 keys, 32 heads of 64 over 8, 20 us, 3.0 TB/s: shares of 600 to 1100 keys behind 4 to 5 us of start and end;
-// one token over 131072 keys, 8 heads over 1, 16.5 us: 254 shares take 5 us for their keys, 3 to find them, 6 to fold them.  A
-// workgroup finds its share in about 2 us (some 600 dependent instructions and a trip to memory).  32 rows a tile, 16 heads over 2: 64 rows
-// over 32768 keys 47 us (365 TFLOP/s); 2 x 509 rows and 22 single tokens over 700 to 6000 keys 37 to 40 us (up to 330), vector instructions in
-// 52 %, matrix instructions in 16 % of the cycles, and workgroups that end between 32 and 40 us.
+// Measured (bf16): 40 single tokens over 500 to 8192 keys, 13 heads of 128, 44.6 us, 4.1 TB/s of the cache (a large copy reaches 4.9);
+// 48 x 2 rows over 300 to 8192 keys, 32 heads of 64 over 8, 21.7 us, 2.8 TB/s: shares of 600 to 1100 keys behind 4 to 5 us of start and end;
+// one token over 131072 keys, 8 heads over 1, 16.9 us: 254 shares take 2 us to be found (some 600 dependent instructions and a trip to
+// memory), 5 for their keys, 1 to be parked and 5 to be folded in two rounds.  32 rows a tile, 16 heads over 2: 64 rows over 32768 keys 46 us
+// (370 TFLOP/s); 2 x 509 rows and 22 single tokens over 700 to 6000 keys 37 to 40 us (up to 330), vector instructions in 50 %, matrix
+// instructions in 16 % of the cycles, and workgroups that end between 32 and 40 us: every tile unpacks its request's keys again, 128
+// tiles of 32 rows those of a 509-row chunk.  fp32: 40 single tokens of 4000 keys, 13 heads, 63 to 76 us; 512 rows of 4096 keys, 8 heads over 1,
+// 40; 512 of 2000, 13 heads, 34; heads of 64, 32 over 8, 2048 of 2048 91.
 #include "kv4.h"
 
 #include <algorithm>
@@ -626,9 +628,11 @@ hipError_t iso_launch_attn_kv4(int dtype, const void *q, int q_stride, const iso
     const unsigned mul = (unsigned)(((((u64)1 << bits) - G) << 32) / G) + 1;
     const line_args a{q, out, nullptr, nullptr, kv4_view_of(cache), b, q_stride, nq, nkv, (int)G, mul, bits, most};
     // Two blocks of rows a tile where a request can have more than one, and, with heads of 128 (two workgroups on a compute unit then instead
-    // of three, pieces twice as large), where a workgroup's share is about 900 keys or more by the room that the table has.  16 and 32
-    // rows a tile, 16 heads over 2: 5 rows for each of 8 requests of up to 4000 keys 14 and 22 us; 509 rows of 700 / 2048 / 6000 17 / 30 / 62 and
-    // 19 / 28 / 54; heads of 64, 32 over 8: 200 rows of 2048 23 and 20, 500 of 500 19 and 16.
+    // of three, pieces twice as large), where a workgroup's share is about 900 keys or more by the room that the table has (not by the keys that
+    // are there, which the host does not know: 8 x 5 rows of up to 4000 keys, 16 heads over 2, 15 us through a table of that width, 19 through
+    // one of 131072).  16 and 32 rows a tile, 16 heads over 2: 5 rows for each of 8 requests of up to 4000 keys 14 and 22 us; 509 rows of
+    // 700 / 2048 / 6000 17 / 30 / 62 and 19 / 28 / 54.  Heads of 64, 32 over 8: 256 rows of 512 / 2048 / 8192 15 / 25 / 58 and 17 / 24 / 52, 2048 of 2048 72 and
+    // 62; 16 over 16: 256 of 512 / 32768 12 / 96 and 13 / 86.
     const long long keys = (long long)b.max_pages * cache.page, pairs = (long long)b.total_rows * nq;
     const bool two = std::min((long long)max_rows * a.G, (long long)most) > 16 && (d == 64 || pairs / 32 * keys >= 900ll * wg_per_cu(2, 128, 2) * iso_num_cu());
     if (dtype == ISO_F32) return d == 64 ? launch<float, 64, 1>(a, ws, s) : launch<float, 128, 1>(a, ws, s);

@@ -1,4 +1,5 @@
-// Attention over the paged 4-bit cache for many rows (bf16): chunks of prompts.  Bound by the matrix cores.
+// Attention over the paged 4-bit cache for many rows (bf16): chunks of prompts.  Bound by the instructions of the softmax and of unpacking
+// beside the matrix cores: both pipes are busy half of the time, one after the other more than at once.
 //
 // A row tile is up to 128 (token, query head) pairs of one key head, whole tokens, 32 rows a wave.  All of a key head's queries share a
 // tile, so the cache is unpacked once for them: tiles of 64 keys go from the pages to registers (requested one tile ahead), are unpacked
@@ -13,8 +14,9 @@
 // request's length on the line is a closed form and a place's tile the root of a quadratic.  Shares begin at multiples of 64 keys of a tile.
 // Pieces of a tile are parked and folded in order by the last to arrive.
 //
-// Measured: 8 heads over 1, 2048 rows over 32768 keys 266 to 321 us (1000 to 830 TFLOP/s, the first after a pause of the card), over 131072 keys 1070
-// (990); 16 heads over 2, 8192 of 8192 350 (790).  In the first vector instructions take 52 %, matrix instructions 48 % of the cycles; products
+// Measured: 8 heads over 1, 2048 rows over 32768 keys 266 to 321 us (1000 to 830 TFLOP/s, the first after a pause of the card), over 131072 keys 1065
+// (990); 16 heads over 2, 8192 of 8192 301 to 350 (910 to 790).  Heads of 64 (two terms a probability), 32 over 8: 2048 rows of 2048 47 (370), over
+// 32768 keys 905 (590).  In the first vector instructions take 52 %, matrix instructions 48 % of the cycles; products
 // of 8192^3 reach 1500 TFLOP/s here, the framework's bf16 attention 960 on the same rows and keys.
 #include "kv4.h"
 #include <type_traits>

@@ -903,17 +903,25 @@ int check_kv4(const iso_kv4 *c) {
     return ISO_OK;
 }
 
-// Which kernels a batch needs, and their regions of its workspace (both are there whatever the call's max_rows and table).  Long chunks
-// deep in a cache go to the tiles of 128 rows, everything else to the line of 16 or 32 rows a tile.  What there is to do is taken to be
-// (row, head) pairs times the keys that the table has room for.  One request (us, tiles of 128 rows and the line):
+// Which kernels a batch needs, and their regions of its workspace (both are there whatever the call's max_rows and table).  Chunks with
+// much to do go to the tiles of 128 rows, everything else to the line of 16 or 32 rows a tile.  What there is to do is taken to be
+// (row, head) pairs times the keys that the table has room for: more than 2^25 of one request, 2^27 of several.  One request (us, tiles of
+// 128 rows and the line):
 //   16 heads over 2:  512 rows of 2048 / 4096 / 32768 keys   36 / 44 / 169 and 28 / 42 / 209;  2000 of 2000  41 and 50
 //                     128 / 256 rows of 32768                85 / 98 and 68 / 115;             16 of 8192    47 and 20
 //   8 heads over 1:   2048 rows of 2048 / 8192 / 32768       34 / 86 / 321 and 33 / 111 / 416
 //   13 heads over 13: 640 rows of 2048 / 4096, 2047 of 2047  34 / 42 / 38 and 28 / 41 / 45
+//   heads of 64, 32 over 8:   128 rows of 2048 / 8192 / 32768  20 / 37 / 80 and 19 / 34 / 88;   512 of 512 / 2048 / 8192  19 / 29 / 72 and 16 / 32 / 86;
+//                             2048 of 2048 / 32768  47 / 905 and 62 / 1066
+//   heads of 64, 8 over 1:    512 rows of 2048 / 8192 / 32768  23 / 38 / 80 and 18 / 32 / 86;   2048 of 2048 / 4096 / 32768  26 / 38 / 238 and 24 / 45 / 284
+//   heads of 64, 16 over 16:  256 rows of 2048 / 32768  20 / 78 and 18 / 86;   512 of 512 / 4096  15 / 29 and 14 / 31;   2048 of 2048  31 and 37
+// (around 2^25, where the line is taken, either may be 10 % ahead: 512 of 2048 with 32 over 8 is the line's, 8 over 1 2048 of 2048 too)
 // Of several requests those of up to SHORT_PAIRS pairs of a key head stay with the line.  Where max_rows allows no others there is no second
 // launch: it would find nothing to do (13 heads over 13, 2 x 400 rows of 2000 keys in a wide table 33.4 us with it, 31.2 without; 32 heads
 // of 64 over 8, 2 x 250 rows of 8000 keys 87 and 84).  22 single tokens (16 heads over 2) and
 //   2 x 512 rows of up to 6000 / 20000 keys  59 / 109 and 51 / 117;  4 x 512 of up to 8192  103 and 116;  1024 of up to 6000  49 and 35
+//   heads of 64, 32 over 8: 2 x 512 of up to 3000 / 6000 / 20000 41 / 56 / 126 and 36 / 57 / 146;  2 x 256 of up to 6000 43 and 34;  2 x 2000
+//   of 2000 alone 82 and 106
 constexpr int SHORT_PAIRS = 1023;
 struct Kv4Launch {
     bool line, rows;

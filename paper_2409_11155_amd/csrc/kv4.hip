@@ -107,7 +107,9 @@ __global__ __launch_bounds__(BT_THREADS) void block_tables_kernel(bt_args a) {
 // Eight elements a lane and half a head: a lane has elements 8 l .. 8 l + 7 of the low half and of the high half of one head (the
 // two that a rotary step joins), four neighbouring lanes have a block of each.  Bound by memory: 16 bytes (bf16) a load, four bytes
 // of codes a store.  bf16, 13 heads of 128: 16384 rows stored in 30 us (4.6 TB/s), loaded in 27; 2047 rows rotated and written
-// in 9.8 (3.3 TB/s), loaded in 5.8 (2.9).  64 rows 4.0 and 2.5: launch and two dependent trips to memory.
+// in 9.8 (3.3 TB/s), loaded in 5.8 (2.9).  64 rows 4.0 and 2.5: launch and two dependent trips to memory.  A rotated head reads its position's
+// cosines and sines again, 512 bytes for 256 of its own (26 times a row with 13 heads; from the caches, but through the same pipe).  fp32:
+// 2047 rows rotated and written in 11.5, 16384 in 96 (4.9 TB/s), stored in 40, loaded in 44.
 template <typename T> __device__ __forceinline__ void load8(const T *p, float (&x)[8]);
 template <> __device__ __forceinline__ void load8<float>(const float *p, float (&x)[8]) {
     const f32x4_t a = reinterpret_cast<const f32x4_t *>(p)[0], b = reinterpret_cast<const f32x4_t *>(p)[1];
