@@ -376,7 +376,7 @@ int iso_kv4_load(iso_ctx *ctx, const iso_kv4 *cache, const int *slots, void *k, 
  *   iso_attn_chunk.  A row that sees no key is zero.  Rows in front of the first request or behind the last are left as they were;
  *   what a cache holds in a token that a row does not see does not reach that row, NaN included.
  *   max_rows: the most rows that one request has, as far as known.  The kernels are chosen by it and by the keys that the table has room
- *   for (a table much wider than the longest request is right, but a chunk may run slower); results are right for any value >= 1.
+ *   for (a table much wider than the longest request is right, but drafts and chunks may run slower); results are right for any value >= 1.
  *   ws: iso_attn_kv4_workspace bytes, zero-filled before its first use (every call leaves it ready for the next call of the same
  *   context, of any shape that fits).  Calls that may overlap in time, replays of a graph among them, need one each.
  *   out and ws must not overlap one another or an input (ISO_ERR_SHAPE; of the table, the first entry is looked at).
